@@ -392,6 +392,126 @@ ibp_status ibp_cache_reset_stats(ibp_cache *c);
  * destroyed marker, so a second ibp_cache_destroy (or any call on it) returns IBP_ESTATE. */
 ibp_status ibp_cache_destroy(ibp_cache *c);
 
+/*
+ * Attention over KV tensors: what reads the rows that the calls above bring to the device
+ * (a row of a KV stream is one token's key or value of one head; Sec. 6.4). Four operators
+ * follow one cache: ibp_attn_prompt (whole prompts), ibp_attn_key_weights (the attention
+ * weight every key received), ibp_attn_decode (one new token per sequence over a paged
+ * cache) and ibp_kv_evict (eviction of the lightest tokens). The paper only names attention
+ * as the consumer; the definitions below are this library's.
+ *
+ * Every call takes device memory of the current HIP device, enqueues its kernels on `stream`
+ * and neither allocates, copies nor synchronizes, so that it may be captured into a graph.
+ * Nothing is kept between calls: intermediate results go to a workspace of the caller's (size
+ * from the _workspace calls, 16-byte aligned, content of no matter), which calls that may
+ * overlap must not share. Lengths, starts and page ids are read on the device and cannot be
+ * checked on the host: they are clamped to the sizes given, so that no wrong value reads or
+ * writes out of bounds. Results are the same for every run: nothing depends on an order of
+ * arrival. The calls check their other arguments as every call does (IBP_EINVAL; IBP_ENOMEM
+ * for an output or workspace that is too small; IBP_EHIP when a launch fails; a call of more
+ * blocks than one launch may have, 2^22, is IBP_EINVAL).
+ */
+enum { IBP_BF16 = 0, IBP_F16 = 1 };      /* ibp_attn.type */
+enum { IBP_ATTN_CAUSAL = 1 };            /* ibp_attn.flags */
+
+typedef struct {
+    uint32_t type;           /* of q, keys, values and out; sums, softmax and lse are fp32 */
+    uint32_t q_heads;        /* a multiple of kv_heads (grouped heads): query head h reads */
+    uint32_t kv_heads;       /*   KV head h / (q_heads / kv_heads) */
+    uint32_t head_dim;       /* a multiple of 8, at most 256 */
+    float scale;             /* of q . k, 1e-30 to 1e30 (usually head_dim^-1/2) */
+    uint32_t flags;          /* IBP_ATTN_CAUSAL or 0 */
+} ibp_attn;
+
+/* Rows [rows][heads][head_dim]: 16-byte aligned, strides in elements, multiples of 8 (row
+ * strides at most 2^23); head_dim itself is contiguous. */
+typedef struct {
+    void *data;
+    uint64_t rows;
+    uint64_t row_stride, head_stride;
+} ibp_rows;
+
+/* A paged cache: key and value pools [n_pages][kv_heads][page_tokens][head_dim] of any
+ * strides (elements, multiples of 8), so that pages of [token][head] order serve too, and
+ * which pages a sequence has: slot i of sequence s is token i % page_tokens of page
+ * d_table[s * table_pages + i / page_tokens]. A slot whose page id is outside [0, n_pages)
+ * counts as absent. */
+typedef struct {
+    void *keys, *values;
+    uint64_t n_pages;
+    uint32_t page_tokens;
+    uint32_t table_pages;    /* page ids per sequence in d_table */
+    const int32_t *d_table;
+    uint64_t key_page_stride, key_head_stride, key_token_stride;
+    uint64_t value_page_stride, value_head_stride, value_token_stride;
+} ibp_pages;
+
+/*
+ * ibp_attn_prompt -- attention of packed sequences: rows [d_q_starts[s], d_q_starts[s + 1])
+ * of q attend to rows [d_k_starts[s], d_k_starts[s + 1]) of k and v (n_seqs + 1 ascending
+ * starts each; any length, zero too). With x_ij = scale q_i . k_j over the keys j that row i
+ * sees (all of its sequence; with IBP_ATTN_CAUSAL j <= i + keys - queries, places inside the
+ * sequence, so that a prompt's last row sees everything before it):
+ *   lse_i = ln sum_j exp(x_ij),   out_i = sum_j exp(x_ij - lse_i) v_j.
+ * A row that sees no key, or only scores of -inf, gives zeros and an lse of -inf. What a row
+ * does not see has no effect on it, infinities and NaN included. d_lse ([q_heads][q rows])
+ * may be null. Rows of q outside all sequences leave out and d_lse as they are.
+ */
+ibp_status ibp_attn_prompt(const ibp_attn *a, const ibp_rows *q, const ibp_rows *k, const ibp_rows *v,
+                           const int32_t *d_q_starts, const int32_t *d_k_starts, uint32_t n_seqs,
+                           const ibp_rows *out, float *d_lse, void *stream);
+
+/*
+ * ibp_attn_key_weights -- the attention weight that every key received:
+ *   d_weights[g][j] = sum over the query heads h of KV head g and the rows i that see key j
+ *                     of exp(x_ij - d_lse[h][i]),
+ * with d_lse as ibp_attn_prompt left it for the same q, k, starts and parameters (a row of
+ * lse -inf gives nothing). d_weights is [kv_heads][k rows]; rows of k outside all sequences
+ * leave theirs as they are. The workspace holds the query heads' own sums (none for
+ * q_heads == kv_heads).
+ */
+ibp_status ibp_attn_key_weights_workspace(uint32_t q_heads, uint32_t kv_heads, uint64_t k_rows, uint64_t *bytes);
+ibp_status ibp_attn_key_weights(const ibp_attn *a, const ibp_rows *q, const ibp_rows *k, const int32_t *d_q_starts,
+                                const int32_t *d_k_starts, uint32_t n_seqs, const float *d_lse, float *d_weights,
+                                void *workspace, uint64_t workspace_bytes, void *stream);
+
+/*
+ * ibp_attn_decode -- attention of one new token per sequence (q: one row per sequence) over
+ * the slots 0 .. d_lens[s] - 1 of its cache, the sums as in ibp_attn_prompt; every slot is
+ * seen, in whatever order its tokens are (so the new token's own key and value are in the
+ * cache already). max_len bounds the lengths (a longer one is taken as max_len; IBP_ERANGE
+ * when the table holds fewer slots). d_lse ([sequences][q_heads]) may be null. d_weights, if
+ * not null, is [sequences][kv_heads][weights_stride]: the sum over the query heads of a KV
+ * head of exp(x - lse) is added to each slot's.
+ */
+ibp_status ibp_attn_decode_workspace(uint32_t n_seqs, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim,
+                                     uint32_t max_len, int weights, uint64_t *bytes);
+ibp_status ibp_attn_decode(const ibp_attn *a, const ibp_rows *q, const ibp_pages *pages, const int32_t *d_lens,
+                           uint32_t max_len, const ibp_rows *out, float *d_lse, float *d_weights,
+                           uint64_t weights_stride, void *workspace, uint64_t workspace_bytes, void *stream);
+
+/*
+ * ibp_kv_evict -- keep m = min(d_lens[s], budget) slots of every (sequence, KV head), each
+ * head its own: those holding the `recent` newest positions (position >= d_next[s] - recent,
+ * d_next[s] being the position after the newest), then the heaviest by d_weights, ties to
+ * the lowest slot (NaN ranks as -inf). Kept slots below m stay in place; the k-th freed slot
+ * below m takes over the k-th kept slot from m on: its key and value rows, weight and
+ * position. So a cache stays dense in its first m slots with the fewest rows moved, tokens
+ * in no particular order, which attention does not mind. d_weights and d_positions (distinct
+ * within a head) are [sequences][kv_heads][stride], the new ones [sequences][kv_heads]
+ * [new_stride] and may be the same arrays (of the same stride); of them the first m slots are
+ * written. d_new_lens[s] = m may be d_lens. Pages must not be shared between sequences. Of
+ * `a` the type, kv_heads and head_dim are used (a valid q_heads and scale still given).
+ * recent <= budget, budget >= 1.
+ */
+ibp_status ibp_kv_evict_workspace(uint32_t n_seqs, uint32_t kv_heads, uint32_t max_len, uint32_t budget,
+                                  uint64_t *bytes);
+ibp_status ibp_kv_evict(const ibp_attn *a, const ibp_pages *pages, const int32_t *d_lens, uint32_t n_seqs,
+                        uint32_t max_len, uint32_t budget, uint32_t recent, const int32_t *d_next,
+                        const float *d_weights, const int32_t *d_positions, uint64_t stride, float *d_new_weights,
+                        int32_t *d_new_positions, uint64_t new_stride, int32_t *d_new_lens, void *workspace,
+                        uint64_t workspace_bytes, void *stream);
+
 /* ibp_last_error -- message of the last failed call on this thread ("" if none).
  * Library plumbing (the paper defines no error reporting). */
 const char *ibp_last_error(void);

@@ -93,7 +93,9 @@ _SIGS = {
     "ibp_cache_reset_stats": [_vp],
     "ibp_cache_destroy": [_vp],
 }
-EXPORTS = sorted(list(_SIGS) + ["ibp_last_error", "ibp_version"])
+_ATTENTION = ("ibp_attn_prompt", "ibp_attn_key_weights_workspace", "ibp_attn_key_weights", "ibp_attn_decode_workspace",
+              "ibp_attn_decode", "ibp_kv_evict_workspace", "ibp_kv_evict")     # in attention.py, on torch tensors
+EXPORTS = sorted(list(_SIGS) + list(_ATTENTION) + ["ibp_last_error", "ibp_version"])
 
 
 def lib():
@@ -384,3 +386,19 @@ def ibp_cache_destroy(c):
         if st != IBP_ESTATE:      # the cache is freed on every other outcome
             c.ptr = None
         _check(st, "ibp_cache_destroy")
+
+
+def __getattr__(name):
+    """The attention operators need torch's tensors, which the rest of the binding does not: they are
+    loaded when first asked for."""
+    if name in _ATTENTION or name in ("IBP_BF16", "IBP_F16", "IBP_ATTN_CAUSAL"):
+        from . import attention
+        if attention.lib is None:
+            for f, args in attention.SIGS.items():
+                getattr(lib(), f).argtypes = args
+                getattr(lib(), f).restype = ctypes.c_int
+            attention.lib, attention.check = lib, _check
+        for n in (*_ATTENTION, "IBP_BF16", "IBP_F16", "IBP_ATTN_CAUSAL"):
+            globals()[n] = getattr(attention, n)
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -2,8 +2,8 @@
 
     python -m paper_2605_30728_amd.build      # or build() from Python
 
-Device code is compiled with packed FP32 instructions disabled (none of the kernels
-do floating point, and the flag keeps hipcc from emitting them anywhere).
+Device code is compiled with packed FP32 instructions disabled: the decompression kernels do
+no floating point, and the attention kernels must not use them.
 """
 import os
 import subprocess
@@ -17,7 +17,9 @@ BUILD_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libibp.so")
 ARCH = os.environ.get("IBP_OFFLOAD_ARCH", "gfx950")
 
-HIP_SOURCES = ["ibp_kernels.hip", "ibp_gather_kernels.hip", "ibp_part_kernels.hip", "ibp_cache_kernels.hip", "ibp_runtime.hip"]
+HIP_SOURCES = ["ibp_kernels.hip", "ibp_gather_kernels.hip", "ibp_part_kernels.hip", "ibp_cache_kernels.hip", "ibp_runtime.hip",
+               "ibp_attn_prompt.hip", "ibp_attn_weights.hip", "ibp_attn_decode.hip", "ibp_kv_evict.hip",
+               "ibp_attn_api.hip"]
 CXX_SOURCES = ["ibp_host.cpp", "ibp_pool.cpp", "ibp_meta_slots.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", f"-I{INCLUDE}", f"-I{CSRC}"]

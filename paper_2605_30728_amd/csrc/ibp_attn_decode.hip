@@ -1,0 +1,368 @@
+// Attention of one new token per sequence over a paged KV cache.
+//
+// The cache's length is split over blocks, and within a block over its waves; each wave runs
+// through its slots 32 at a time with a running reference and sum, a block joins its waves, and
+// a second kernel joins the blocks of a sequence:
+//   m = max_x m_x,  l = sum_x l_x 2^(m_x - m),  out = sum_x acc_x 2^(m_x - m) / l.
+// Where the slots' accumulated weights are asked for, the scores are kept and the second kernel
+// adds exp(s - lse) of every slot, in the order of the query heads.
+#include "ibp_attn.hpp"
+#include "ibp_attn_wave.hpp"
+
+#include <algorithm>
+
+namespace ibp {
+namespace attn {
+
+namespace {
+
+using namespace dev;
+
+struct DecodeArgs {
+    Rows q, out;
+    Pages pg;
+    const int32_t *lens;
+    float *lse, *weights;
+    uint64_t weights_stride;
+    float *stats;                // [n_seqs][q_heads][splits] pairs: reference (in scores) and sum
+    float *partial;              // [n_seqs][q_heads][splits][dim]
+    float *scores;               // [n_seqs][q_heads][scores_stride], null: not asked for
+    uint32_t scores_stride;
+    uint32_t n_seqs, q_heads, kv_heads, group, head_blocks, dim, max_len;
+    uint32_t split_tokens, splits;
+    float scale, scale_log2;
+};
+
+constexpr int kWaves = 4;
+constexpr int kChunk = 32;
+
+__device__ __forceinline__ int slots_of(const DecodeArgs &a, uint32_t seq) {
+    return min(max(a.lens[seq], 0), (int)a.max_len);
+}
+
+template <class T, int DIM>
+__global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_decode(DecodeArgs a) {
+    constexpr int KS = DIM / 32, DT = DIM / 16, RB = Tile<DIM>::kRowBytes, CH = Tile<DIM>::kChunks;
+    constexpr int kChunkBytes = kChunk * RB, VL = kChunkBytes / 1024, kRowsPer = 64 / CH;
+    constexpr int kJoin = 16 * (DIM + 4) * 4;        // a wave's sums, for the join
+    constexpr int kWaveBytes = kChunkBytes > kJoin ? kChunkBytes : kJoin;
+    __shared__ __align__(128) uint8_t lds[kWaves * kWaveBytes];
+    __shared__ float stat[kWaves][2][16];
+
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), quarter = lane >> 4, col = lane & 15;
+    const uint32_t hb = blockIdx.x % (a.kv_heads * a.head_blocks), rest = blockIdx.x / (a.kv_heads * a.head_blocks);
+    const uint32_t split = rest % a.splits, seq = rest / a.splits;
+    const uint32_t kv = hb / a.head_blocks, head0 = kv * a.group + hb % a.head_blocks * 16;
+    const int heads = min((int)((kv + 1) * a.group - head0), 16);
+    const int len = uniform(slots_of(a, seq));
+    const int from = split * a.split_tokens, to = min(len, from + (int)a.split_tokens);
+    if (from >= to && !(split == 0)) return;
+
+    Frag q[KS];
+    {
+        const uint8_t *qp = (const uint8_t *)a.q.data + ((int64_t)seq * a.q.row + (int64_t)(head0 + min(col, heads - 1)) * a.q.head) * 2;
+#pragma unroll
+        for (int x = 0; x < KS; ++x) {
+            const int d = x * 32 + quarter * 8;
+            q[x] = Frag{0, 0, 0, 0};
+            if (d < (int)a.dim) q[x] = *reinterpret_cast<const Frag *>(qp + d * 2);
+        }
+    }
+
+    const int32_t *table = a.pg.table + (int64_t)seq * a.pg.table_stride;
+    // a slot's page and place in it, and whether there is such a page
+    auto find = [&](int slot, int &page, int &place) {
+        const uint32_t s = min(slot, len - 1);
+        const uint32_t i = a.pg.page_magic ? __umulhi(s, a.pg.page_magic) >> a.pg.page_shift : s >> a.pg.page_shift;
+        place = (int)(s - i * a.pg.page_tokens);
+        const int32_t p = table[i];
+        const bool there = slot < len && (uint32_t)p < a.pg.n_pages;
+        page = (uint32_t)p < a.pg.n_pages ? p : 0;
+        return there;
+    };
+
+    const float inf = __builtin_inff();
+    const float c = a.scale_log2;
+    float m = -inf, l = 0.f;
+    f32x4 acc[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d) acc[d] = f32x4{};
+    uint8_t *vt = lds + wave * kWaveBytes;
+
+    Frag kf[2][KS], vf[VL];
+    uint64_t live = 0;                   // bit i: slot i of the chunk is there
+    auto load = [&](int chunk) {
+        int page, place;
+        const bool there = find(chunk + (lane & 31), page, place);
+        live = __ballot(there) & 0xffffffffull;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int at = j * 16 + col;
+            const uint8_t *kp = (const uint8_t *)a.pg.k.data + ((int64_t)__shfl(page, at) * a.pg.k.page + (int64_t)__shfl(place, at) * a.pg.k.token +
+                                                                (int64_t)kv * a.pg.k.head) * 2;
+#pragma unroll
+            for (int x = 0; x < KS; ++x) {
+                const int d = x * 32 + quarter * 8;
+                kf[j][x] = Frag{0, 0, 0, 0};
+                if (d < (int)a.dim) kf[j][x] = *reinterpret_cast<const Frag *>(kp + d * 2);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < VL; ++i) {
+            const int row = i * kRowsPer + lane / CH, ch = lane % CH;
+            const uint8_t *vp = (const uint8_t *)a.pg.v.data + ((int64_t)__shfl(page, row) * a.pg.v.page + (int64_t)__shfl(place, row) * a.pg.v.token +
+                                                                (int64_t)kv * a.pg.v.head) * 2;
+            vf[i] = Frag{0, 0, 0, 0};
+            if (ch * 8 < (int)a.dim && (live >> row & 1)) vf[i] = *reinterpret_cast<const Frag *>(vp + ch * 16);
+        }
+    };
+
+    int chunk = from + wave * kChunk;
+    if (chunk < to) load(chunk);
+    for (; chunk < to; chunk += kWaves * kChunk) {
+        f32x4 s[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            s[j] = f32x4{};
+#pragma unroll
+            for (int x = 0; x < KS; ++x) s[j] = T::mfma16(kf[j][x], q[x], s[j]);
+        }
+#pragma unroll
+        for (int i = 0; i < VL; ++i) {
+            const int row = i * kRowsPer + lane / CH, ch = lane % CH;
+            *reinterpret_cast<Frag *>(vt + row * RB + ((ch ^ Tile<DIM>::columns(row)) << 4)) = vf[i];
+        }
+        const uint64_t now = live;
+        if (chunk + kWaves * kChunk < to) load(chunk + kWaves * kChunk);
+
+        if (now != 0xffffffffull) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (!(now >> (j * 16 + quarter * 4 + i) & 1)) s[j][i] = -inf;
+        }
+        if (a.scores && col < heads) {
+            float *sp = a.scores + ((int64_t)seq * a.q_heads + head0 + col) * a.scores_stride + chunk + quarter * 4;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) *reinterpret_cast<f32x4 *>(sp + j * 16) = s[j];
+        }
+        float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
+                          fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+        top = max_halves(max_quarters(top));
+        if (__any(top > m)) {
+            const float next = fmaxf(m, top);
+            const float keep = m == -inf ? 0.f : exp2_fast((m - next) * c);
+            l *= keep;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) acc[d] *= keep;
+            m = next;
+        }
+        const float mc = m == -inf ? 0.f : m * c;
+        Frag p;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[j][i] = exp2_fast(__builtin_fmaf(s[j][i], c, -mc));
+                l += s[j][i];
+            }
+            p[j * 2] = T::pack(s[j][0], s[j][1]);
+            p[j * 2 + 1] = T::pack(s[j][2], s[j][3]);
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+            const int key = quarter * 4 + (col >> 2), at = d * 16 + (col & 3) * 4;
+            const u32x2 lo = read_columns<DIM>(vt, key, at), hi = read_columns<DIM>(vt, key + 16, at);
+            acc[d] = T::mfma16(Frag{lo[0], lo[1], hi[0], hi[1]}, p, acc[d]);
+        }
+    }
+
+    // the block's waves joined: lane's column is a head, its registers dims quarter * 4 + i
+    l = sum_halves(sum_quarters(l));
+    if (quarter == 0) {
+        stat[wave][0][col] = m;
+        stat[wave][1][col] = l;
+    }
+    __syncthreads();
+    float *mine = reinterpret_cast<float *>(vt);
+#pragma unroll
+    for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4 *>(mine + col * (DIM + 4) + d * 16 + quarter * 4) = acc[d];
+    __syncthreads();
+    const int h = threadIdx.x >> 4;          // 16 heads, 16 threads each
+    if (h >= heads) return;
+    float top = -inf, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, stat[w][0][h]);
+    float part[kWaves];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        part[w] = stat[w][0][h] == -inf ? (stat[w][1][h] == 0.f ? 0.f : 1.f) : exp2_fast((stat[w][0][h] - top) * c);
+        sum += part[w] * stat[w][1][h];
+    }
+    const uint32_t head = head0 + h;
+    const bool last = a.splits == 1;
+    const float inv = !last ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+    for (int d = (threadIdx.x & 15) * 4; d < (int)a.dim; d += 64) {
+        f32x4 x{};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w)
+            if (part[w] != 0.f) x += part[w] * *reinterpret_cast<const f32x4 *>(reinterpret_cast<float *>(lds + w * kWaveBytes) + h * (DIM + 4) + d);
+        x *= inv;
+        if (last) {
+            u32x2 o;
+            o[0] = T::pack(x[0], x[1]);
+            o[1] = T::pack(x[2], x[3]);
+            *reinterpret_cast<u32x2 *>((uint8_t *)a.out.data + ((int64_t)seq * a.out.row + (int64_t)head * a.out.head + d) * 2) = o;
+        } else {
+            *reinterpret_cast<f32x4 *>(a.partial + (((int64_t)seq * a.q_heads + head) * a.splits + split) * a.dim + d) = x;
+        }
+    }
+    if ((threadIdx.x & 15) == 0) {
+        if (last && a.lse) a.lse[(int64_t)seq * a.q_heads + head] = sum == 0.f ? -inf : top * a.scale + __logf(sum);
+        if (!last || a.weights) {
+            float *st = a.stats + (((int64_t)seq * a.q_heads + head) * a.splits + split) * 2;
+            st[0] = top;
+            st[1] = sum;
+        }
+    }
+}
+
+// The splits of a sequence that a head has, and their joint reference and sum.
+__device__ __forceinline__ void join_stats(const DecodeArgs &a, uint32_t seq, uint32_t head, uint32_t n, float &top, float &sum) {
+    const int lane = threadIdx.x & 63;
+    const float *st = a.stats + ((int64_t)seq * a.q_heads + head) * a.splits * 2;
+    const float inf = __builtin_inff();
+    top = -inf;
+    for (uint32_t x = lane; x < n; x += 64) top = fmaxf(top, st[x * 2]);
+    for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
+    sum = 0.f;
+    for (uint32_t x = lane; x < n; x += 64)
+        sum += st[x * 2] == -inf ? st[x * 2 + 1] : st[x * 2 + 1] * exp2_fast((st[x * 2] - top) * a.scale_log2);
+    for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x);
+}
+
+constexpr int kJoinSlots = 1024;             // slots whose weights a block of the second kernel adds
+
+// Block 0 of a (sequence, KV head) joins the splits of its query heads, a wave each in turn; the
+// others add the weights of kJoinSlots slots.
+template <class T>
+__global__ __launch_bounds__(256) void k_attn_decode_join(DecodeArgs a, uint32_t weight_blocks) {
+    const uint32_t per = weight_blocks + (a.splits > 1 ? 1 : 0);
+    const uint32_t x = blockIdx.x % per, kv = blockIdx.x / per % a.kv_heads, seq = blockIdx.x / per / a.kv_heads;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int len = slots_of(a, seq);
+    const uint32_t n = len > 0 ? (len + a.split_tokens - 1) / a.split_tokens : 1;
+    const float inf = __builtin_inff();
+    if (x == weight_blocks) {
+        for (uint32_t g = wave; g < a.group; g += 4) {
+            const uint32_t head = kv * a.group + g;
+            float top, sum;
+            join_stats(a, seq, head, n, top, sum);
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            const float *st = a.stats + ((int64_t)seq * a.q_heads + head) * a.splits * 2;
+            const float *pp = a.partial + ((int64_t)seq * a.q_heads + head) * a.splits * a.dim;
+            for (int d = lane * 2; d < (int)a.dim; d += 128) {
+                f32x2 o{};
+                for (uint32_t y = 0; y < n; ++y) {
+                    if (st[y * 2 + 1] == 0.f) continue;
+                    const float f = st[y * 2] == -inf ? 1.f : exp2_fast((st[y * 2] - top) * a.scale_log2);
+                    o += f * *reinterpret_cast<const f32x2 *>(pp + (int64_t)y * a.dim + d);
+                }
+                *reinterpret_cast<uint32_t *>((uint8_t *)a.out.data + ((int64_t)seq * a.out.row + (int64_t)head * a.out.head + d) * 2) =
+                    T::pack(o[0] * inv, o[1] * inv);
+            }
+            if (a.lse && lane == 0) a.lse[(int64_t)seq * a.q_heads + head] = sum == 0.f ? -inf : top * a.scale + __logf(sum);
+        }
+        return;
+    }
+    const int slot0 = x * kJoinSlots + threadIdx.x * 4;
+    if ((int)(x * kJoinSlots) >= len) return;
+    float w[4] = {};
+    for (uint32_t g = 0; g < a.group; ++g) {
+        const uint32_t head = kv * a.group + g;
+        float top, sum;
+        join_stats(a, seq, head, n, top, sum);
+        const float inv = sum == 0.f ? 0.f : 1.f / sum, mc = top == -inf ? 0.f : top * a.scale_log2;
+        if (slot0 < len) {
+            const f32x4 s = *reinterpret_cast<const f32x4 *>(a.scores + ((int64_t)seq * a.q_heads + head) * a.scores_stride + slot0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] += exp2_fast(__builtin_fmaf(s[i], a.scale_log2, -mc)) * inv;
+        }
+    }
+    float *out = a.weights + ((int64_t)seq * a.kv_heads + kv) * a.weights_stride + slot0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (slot0 + i < len) out[i] += w[i];
+}
+
+template <class T>
+void decode_of(const DecodeArgs &a, uint32_t blocks, hipStream_t stream) {
+    const dim3 grid(blocks), block(64 * kWaves);
+    if (a.dim <= 64) k_attn_decode<T, 64><<<grid, block, 0, stream>>>(a);
+    else if (a.dim <= 96) k_attn_decode<T, 96><<<grid, block, 0, stream>>>(a);
+    else if (a.dim <= 128) k_attn_decode<T, 128><<<grid, block, 0, stream>>>(a);
+    else k_attn_decode<T, 256><<<grid, block, 0, stream>>>(a);
+}
+
+uint64_t up256(uint64_t x) { return (x + 255) / 256 * 256; }
+
+}  // namespace
+
+DecodePlan plan_decode(uint32_t n_seqs, uint32_t q_heads, uint32_t kv_heads, uint32_t dim, uint32_t max_len,
+                       bool weights) {
+    DecodePlan p{};
+    p.head_blocks = (q_heads / kv_heads + 15) / 16;
+    // enough blocks to fill the chip, of at least 128 slots (one chunk per wave)
+    const uint64_t rows = std::max<uint64_t>((uint64_t)n_seqs * kv_heads * p.head_blocks, 1);
+    const uint64_t want = (1024 + rows - 1) / rows;
+    uint64_t t = (std::max<uint64_t>(max_len, 1) + want - 1) / want;
+    t = std::max<uint64_t>((t + 127) / 128 * 128, 128);
+    p.split_tokens = (uint32_t)t;
+    p.splits = (uint32_t)((std::max<uint64_t>(max_len, 1) + t - 1) / t);
+    const uint64_t parts = (uint64_t)n_seqs * q_heads * p.splits;
+    p.stats_off = 0;
+    p.out_off = up256(parts * 8);
+    p.scores_off = p.out_off + (p.splits > 1 ? up256(parts * dim * 4) : 0);
+    p.bytes = p.scores_off + (weights ? up256((uint64_t)n_seqs * q_heads * ((max_len + 31ull) / 32 * 32) * 4) : 0);
+    return p;
+}
+
+hipError_t launch_decode(const Shape &s, const Rows &q, const Pages &pg, const int32_t *lens, uint32_t n_seqs,
+                         uint32_t max_len, const Rows &out, float *lse, float *weights, uint64_t weights_stride,
+                         const DecodePlan &plan, uint8_t *workspace, hipStream_t stream) {
+    if (n_seqs == 0) return hipSuccess;
+    const uint64_t blocks = (uint64_t)n_seqs * plan.splits * s.kv_heads * plan.head_blocks;
+    const uint32_t weight_blocks = weights ? (max_len + kJoinSlots - 1) / kJoinSlots : 0;
+    const uint64_t join = (uint64_t)n_seqs * s.kv_heads * (weight_blocks + (plan.splits > 1 ? 1 : 0));
+    if (blocks > kMaxGrid || join > kMaxGrid) return hipErrorInvalidConfiguration;
+    DecodeArgs a{q, out, pg, lens, lse, weights, weights_stride, (float *)(workspace + plan.stats_off),
+                 (float *)(workspace + plan.out_off), weights ? (float *)(workspace + plan.scores_off) : nullptr,
+                 (max_len + 31) / 32 * 32, n_seqs, s.q_heads, s.kv_heads, s.group, plan.head_blocks, s.dim, max_len,
+                 plan.split_tokens, plan.splits, s.scale, s.scale_log2};
+    if (s.f16) decode_of<F16>(a, (uint32_t)blocks, stream);
+    else decode_of<Bf16>(a, (uint32_t)blocks, stream);
+    if (join) {
+        if (s.f16) k_attn_decode_join<F16><<<dim3((uint32_t)join), dim3(256), 0, stream>>>(a, weight_blocks);
+        else k_attn_decode_join<Bf16><<<dim3((uint32_t)join), dim3(256), 0, stream>>>(a, weight_blocks);
+    }
+    return hipGetLastError();
+}
+
+void page_division(uint32_t page_tokens, uint32_t &magic, uint32_t &shift) {
+    // d = page_tokens > 1 not a power of two, k = ceil(log2 d): with magic = ceil(2^(31 + k) / d)
+    // (below 2^32, since 2^k < 2 d), n magic / 2^(31 + k) exceeds n / d by less than
+    // n / 2^(31 + k) <= 1 / 2^k <= 1 / d for n < 2^31, so its floor is n / d's
+    uint32_t k = 0;
+    while ((1ull << k) < page_tokens) ++k;
+    if ((1ull << k) == page_tokens) {
+        magic = 0;
+        shift = k;
+        return;
+    }
+    magic = (uint32_t)(((1ull << (31 + k)) + page_tokens - 1) / page_tokens);
+    shift = k - 1;
+}
+
+}  // namespace attn
+}  // namespace ibp

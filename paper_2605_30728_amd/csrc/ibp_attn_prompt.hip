@@ -1,0 +1,273 @@
+// Attention over whole prompts.
+//
+// Row i of a sequence with keys k_j and values v_j: with s_ij = scale * q_i . k_j over the keys
+// that i sees,  out_i = sum_j exp(s_ij) v_j / sum_j exp(s_ij)  and  lse_i = ln sum_j exp(s_ij),
+// in one pass over the keys with a running reference m and a running sum: what has been added up
+// so far is scaled by exp(m_old - m_new) when the reference moves.
+#include "ibp_attn.hpp"
+#include "ibp_attn_wave.hpp"
+
+namespace ibp {
+namespace attn {
+
+namespace {
+
+using namespace dev;
+
+struct PromptArgs {
+    Rows q, k, v, out;
+    Packed p;
+    float *lse;
+    uint32_t q_heads, kv_heads, group, dim;
+    uint32_t tiles;              // blocks per head: at least the tiles of all sequences
+    float scale, scale_log2;
+    uint32_t causal;
+};
+
+constexpr int kWaves = 4;
+constexpr int kBlockRows = 32 * kWaves;
+constexpr float kLazy = 8.f;     // how far (in powers of two) weights may exceed 1
+
+template <int DIM>
+constexpr int key_tile() { return DIM <= 128 ? 64 : 32; }
+
+// One row, key by key in 32 bits, by one wave: lanes are keys for the scores and columns for the
+// sum. Only for rows whose tiles hold infinities or NaN in places that the row does not see.
+template <class T, int DIM>
+__device__ void attend_row(const PromptArgs &a, int row, int head, const uint8_t *kp, const uint8_t *vp, int keys) {
+    const int lane = threadIdx.x & 63;
+    const uint16_t *q = (const uint16_t *)a.q.data + (int64_t)row * a.q.row + (int64_t)head * a.q.head;
+    const float inf = __builtin_inff();
+    float m = -inf, l = 0.f, acc[(DIM + 63) / 64] = {};
+    for (int k0 = 0; k0 < keys; k0 += 64) {
+        float s = -inf;
+        if (k0 + lane < keys) {
+            const uint16_t *k = (const uint16_t *)kp + (int64_t)(k0 + lane) * a.k.row;
+            s = 0.f;
+            for (int d = 0; d < (int)a.dim; ++d) s = __builtin_fmaf(T::value(q[d]), T::value(k[d]), s);
+        }
+        float top = s;
+        for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
+        const float next = fmaxf(m, top), keep = m == -inf ? 0.f : exp2_fast((m - next) * a.scale_log2);
+        const float p = exp2_fast(__builtin_fmaf(s, a.scale_log2, next == -inf ? 0.f : -next * a.scale_log2));
+        l *= keep;
+        for (float &x : acc) x *= keep;
+        float sum = p;
+        for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x);
+        l += sum;
+        m = next;
+        for (int j = 0; j < min(keys - k0, 64); ++j) {
+            const uint16_t *v = (const uint16_t *)vp + (int64_t)(k0 + j) * a.v.row;
+            const float w = __shfl(p, j);
+#pragma unroll
+            for (int x = 0; x < (DIM + 63) / 64; ++x)
+                if (lane + 64 * x < (int)a.dim) acc[x] = __builtin_fmaf(w, T::value(v[lane + 64 * x]), acc[x]);
+        }
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    uint16_t *out = (uint16_t *)a.out.data + (int64_t)row * a.out.row + (int64_t)head * a.out.head;
+#pragma unroll
+    for (int x = 0; x < (DIM + 63) / 64; ++x)
+        if (lane + 64 * x < (int)a.dim) out[lane + 64 * x] = (uint16_t)T::pack(acc[x] * inv, 0.f);
+    if (a.lse && lane == 0) a.lse[(int64_t)head * a.p.q_rows + row] = l == 0.f ? -inf : m * a.scale + __logf(l);
+}
+
+template <class T, int DIM>
+__global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_prompt(PromptArgs a) {
+    constexpr int N = key_tile<DIM>(), RB = Tile<DIM>::kRowBytes;
+    constexpr int KS = DIM / 16, DT = DIM / 32, NT = N / 32;
+    constexpr int kTileBytes = N * RB, kLoads = kTileBytes / 1024 / kWaves;
+    __shared__ __align__(128) uint8_t lds[4 * kTileBytes];    // K, V of two tiles
+
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
+
+    // the head and tile of this block: the heads that share keys run on one XCD where they can
+    // be dealt out evenly, tiles with the most keys first
+    uint32_t head, t;
+    const uint32_t b = blockIdx.x;
+    if (a.kv_heads % 8 == 0) {
+        const uint32_t i = b >> 3, per = a.group * a.tiles;
+        head = ((b & 7) + 8 * (i / per)) * a.group + i % per % a.group;
+        t = i % per / a.group;
+    } else {
+        head = b % a.q_heads;
+        t = b / a.q_heads;
+    }
+    SeqTile st;
+    if (!find_tile<false>(a.p.q_starts, a.p.k_starts, a.p.n_seqs, a.p.q_rows, a.p.k_rows, kBlockRows, t, st)) return;
+    const int tile = st.tiles - 1 - st.tile;
+    const int q_len = st.q_len, k_len = st.k_len;
+    const int past = k_len - q_len;                            // causal: row i sees keys j <= i + past
+    const int row = tile * kBlockRows + wave * 32 + col;
+    const int seen_row = min(row, q_len - 1);
+    const int limit = a.causal ? min(max(seen_row + past + 1, 0), k_len) : k_len;   // keys that this lane's row sees
+    const int wave_first = min(tile * kBlockRows + wave * 32, q_len - 1);
+    const int wave_last = min(tile * kBlockRows + wave * 32 + 31, q_len - 1);
+    const int wave_all = a.causal ? min(max(wave_first + past + 1, 0), k_len) : k_len;   // keys that all its rows see
+    const int wave_any = a.causal ? min(max(wave_last + past + 1, 0), k_len) : k_len;    // keys that any of them sees
+    const int block_last = min(tile * kBlockRows + kBlockRows - 1, q_len - 1);
+    const int keys = a.causal ? min(max(block_last + past + 1, 0), k_len) : k_len;
+    const int n_tiles = (keys + N - 1) / N;
+
+    const uint32_t kv = head / a.group;
+    const uint32_t k_stride = (uint32_t)a.k.row * 2, v_stride = (uint32_t)a.v.row * 2;
+    const uint8_t *kp = (const uint8_t *)a.k.data + ((int64_t)st.k0 * a.k.row + (int64_t)kv * a.k.head) * 2;
+    const uint8_t *vp = (const uint8_t *)a.v.data + ((int64_t)st.k0 * a.v.row + (int64_t)kv * a.v.head) * 2;
+
+    uint32_t k_off[kLoads], v_off[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        const int slot = (i * kWaves + wave) * 64 + lane;
+        k_off[i] = tile_source<DIM, true>(slot, k_stride, a.dim);
+        v_off[i] = tile_source<DIM, false>(slot, v_stride, a.dim);
+    }
+    auto load_tile = [&](int n, int buf) {
+        const int rows = min(k_len - n * N, N);
+        const Rsrc kr = descriptor(kp + (int64_t)n * N * k_stride, (rows - 1) * k_stride + a.dim * 2);
+        const Rsrc vr = descriptor(vp + (int64_t)n * N * v_stride, (rows - 1) * v_stride + a.dim * 2);
+        uint8_t *at = lds + buf * 2 * kTileBytes + wave * 1024;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) load_to_lds(kr, at + i * kWaves * 1024, k_off[i]);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) load_to_lds(vr, at + kTileBytes + i * kWaves * 1024, v_off[i]);
+    };
+
+    if (n_tiles > 0) load_tile(0, 0);
+
+    Frag q[KS];
+    {
+        const uint8_t *qp = (const uint8_t *)a.q.data + ((int64_t)(st.q0 + seen_row) * a.q.row + (int64_t)head * a.q.head) * 2;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            const int d = s * 16 + half * 8;
+            q[s] = Frag{0, 0, 0, 0};
+            if (d < (int)a.dim) q[s] = *reinterpret_cast<const Frag *>(qp + d * 2);
+        }
+    }
+
+    const float inf = __builtin_inff();
+    const float c = a.scale_log2, lazy = kLazy / c;
+    float m = -inf, l = 0.f;
+    f32x16 acc[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d) acc[d] = f32x16{};
+
+    bool odd = false;
+    for (int n = 0; n < n_tiles; ++n) {
+        tiles_loaded();
+        if (n + 1 < n_tiles) load_tile(n + 1, (n + 1) & 1);
+        const int key0 = n * N;
+        if (key0 >= wave_any) continue;
+        const uint8_t *kt = lds + (n & 1) * 2 * kTileBytes, *vt = kt + kTileBytes;
+
+        f32x16 s[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            s[j] = f32x16{};
+#pragma unroll
+            for (int x = 0; x < KS; ++x)
+                s[j] = T::mfma32(read_rows<DIM>(kt, j * 32 + col, x * 2 + half), q[x], s[j]);
+        }
+        const bool masked = key0 + N > wave_all;
+        if (masked) {
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (key0 + j * 32 + (i >> 2) * 8 + half * 4 + (i & 3) >= limit) s[j][i] = -inf;
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[j][i]);
+        top = max_halves(top);
+        if (__any(top > m + lazy)) {
+            const float next = fmaxf(m, top);
+            const float keep = m == -inf ? 0.f : exp2_fast((m - next) * c);
+            l *= keep;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) acc[d] *= keep;
+            m = next;
+        }
+        const float mc = m == -inf ? 0.f : m * c;
+        Frag p[NT * 2];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[j][i] = exp2_fast(__builtin_fmaf(s[j][i], c, -mc));
+                l += s[j][i];
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[j * 2 + i / 4][i % 4] = T::pack(s[j][i * 2], s[j][i * 2 + 1]);
+        }
+
+        if (masked) {
+            // a weight of zero must not meet an infinity or NaN: rows that do not see all of such
+            // a tile are done again, key by key
+#pragma unroll 4
+            for (int x = lane * 16; x < kTileBytes; x += 1024)
+                odd |= has_nonfinite<T>(*reinterpret_cast<const Frag *>(vt + x));
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int x = 0; x < NT * 2; ++x) {
+                // 16 keys of 32 columns, in the order of p's keys
+                const int key = (x >> 1) * 32 + (x & 1) * 16 + half * 4 + ((lane & 15) >> 2);
+                const int at = d * 32 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+                const u32x2 lo = read_columns<DIM>(vt, key, at), hi = read_columns<DIM>(vt, key + 8, at);
+                acc[d] = T::mfma32(Frag{lo[0], lo[1], hi[0], hi[1]}, p[x], acc[d]);
+            }
+    }
+    if (__any(odd)) {
+        const int rows = min(q_len - (tile * kBlockRows + wave * 32), 32);
+        for (int r = 0; r < rows; ++r)
+            attend_row<T, DIM>(a, st.q0 + row - col + r, head, kp, vp, uniform(__shfl(limit, r)));
+        return;
+    }
+
+    l = sum_halves(l);
+    if (row >= q_len) return;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    uint8_t *op = (uint8_t *)a.out.data + ((int64_t)(st.q0 + row) * a.out.row + (int64_t)head * a.out.head) * 2;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int at = d * 32 + i * 8 + half * 4;
+            u32x2 w;
+            w[0] = T::pack(acc[d][i * 4] * inv, acc[d][i * 4 + 1] * inv);
+            w[1] = T::pack(acc[d][i * 4 + 2] * inv, acc[d][i * 4 + 3] * inv);
+            if (at < (int)a.dim) *reinterpret_cast<u32x2 *>(op + at * 2) = w;
+        }
+    if (a.lse && half == 0)
+        a.lse[(int64_t)head * a.p.q_rows + st.q0 + row] = l == 0.f ? -inf : m * a.scale + __logf(l);
+}
+
+template <class T>
+hipError_t prompt_of(const PromptArgs &a, uint32_t blocks, hipStream_t stream) {
+    const dim3 grid(blocks), block(64 * kWaves);
+    if (a.dim <= 64) k_attn_prompt<T, 64><<<grid, block, 0, stream>>>(a);
+    else if (a.dim <= 96) k_attn_prompt<T, 96><<<grid, block, 0, stream>>>(a);
+    else if (a.dim <= 128) k_attn_prompt<T, 128><<<grid, block, 0, stream>>>(a);
+    else k_attn_prompt<T, 256><<<grid, block, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_prompt(const Shape &s, const Rows &q, const Rows &k, const Rows &v, const Packed &p, const Rows &out,
+                         float *lse, hipStream_t stream) {
+    if (p.n_seqs == 0 || p.q_rows == 0) return hipSuccess;
+    const uint64_t tiles = p.q_rows / kBlockRows + (uint64_t)p.n_seqs;   // what all sequences need at most
+    const uint64_t blocks = tiles * s.q_heads;
+    if (blocks > kMaxGrid) return hipErrorInvalidConfiguration;
+    PromptArgs a{q, k, v, out, p, lse, s.q_heads, s.kv_heads, s.group, s.dim, (uint32_t)tiles, s.scale, s.scale_log2,
+                 s.causal ? 1u : 0u};
+    return s.f16 ? prompt_of<F16>(a, (uint32_t)blocks, stream) : prompt_of<Bf16>(a, (uint32_t)blocks, stream);
+}
+
+}  // namespace attn
+}  // namespace ibp

@@ -1,0 +1,324 @@
+"""Attention over prompts and the keys' weights against their definition in 64 bits."""
+import pytest
+import torch
+
+from attention_reference import attend, key_weights, visible
+
+pytestmark = pytest.mark.gpu
+NEG = float("-inf")
+BF16, F16 = torch.bfloat16, torch.float16
+
+
+@pytest.fixture(scope="module")
+def ibp():
+    import paper_2605_30728_amd
+    return paper_2605_30728_amd
+
+
+def starts(lengths):
+    return torch.tensor([sum(lengths[:i]) for i in range(len(lengths) + 1)], dtype=torch.int32)
+
+
+def inputs(kind, heads, kv_heads, dim, q_lens, k_lens, seed=0, gain=1.0):
+    g = torch.Generator().manual_seed(seed)
+    new = lambda n, h: torch.randn(n, h, dim, generator=g).mul_(gain).to(kind)  # noqa: E731
+    return new(sum(q_lens), heads), new(sum(k_lens), kv_heads), new(sum(k_lens), kv_heads)
+
+
+def run_prompt(ibp, q, k, v, q_lens, k_lens, causal=True, scale=None, out=None):
+    dq, dk, dv = (x if x.is_cuda else x.cuda() for x in (q, k, v))
+    out = torch.full(q.shape, 7.0, dtype=q.dtype, device="cuda") if out is None else out
+    lse = torch.full((q.shape[1], q.shape[0]), 7.0, device="cuda")
+    ibp.ibp_attn_prompt(dq, dk, dv, starts(q_lens).cuda(), starts(k_lens).cuda(), out, lse, causal=causal, scale=scale)
+    torch.cuda.synchronize()
+    return out.cpu(), lse.cpu()
+
+
+def check_prompt(q, k, v, q_lens, k_lens, out, lse, causal=True, scale=None):
+    scale = q.shape[2] ** -0.5 if scale is None else scale
+    group = q.shape[1] // k.shape[1]
+    q0 = k0 = 0
+    for ql, kl in zip(q_lens, k_lens):
+        rq, rk = slice(q0, q0 + ql), slice(k0, k0 + kl)
+        q0, k0 = q0 + ql, k0 + kl
+        for h in range(q.shape[1]):
+            o, x, o_tol, x_tol = attend(q[rq, h], k[rk, h // group], v[rk, h // group], scale, visible(ql, kl, causal))
+            none = x == NEG
+            assert torch.equal(lse[h, rq] == NEG, none)
+            assert (out[rq, h][none] == 0).all()
+            assert ((lse[h, rq][~none].double() - x[~none]).abs() <= x_tol[~none]).all()
+            off = (out[rq, h].double() - o).abs()
+            assert torch.isfinite(out[rq, h]).all() and (off <= o_tol).all(), (h, (off / o_tol.clamp(min=1e-30)).max())
+
+
+LENGTHS = [([1], [1]), ([33], [33]), ([129, 0, 1, 64, 200], [129, 0, 1, 64, 200]), ([5, 1, 70], [300, 65, 70]),
+           ([40, 130, 3], [7, 100, 0]), ([2], [1500])]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("lens", LENGTHS, ids=[f"q{a}-k{b}".replace(" ", "") for a, b in LENGTHS])
+@pytest.mark.parametrize("kind,heads,kv_heads,dim", [(BF16, 4, 2, 128), (F16, 3, 1, 64), (BF16, 2, 2, 80), (F16, 2, 1, 256)])
+def test_prompt(ibp, kind, heads, kv_heads, dim, lens, causal):
+    q, k, v = inputs(kind, heads, kv_heads, dim, *lens)
+    out, lse = run_prompt(ibp, q, k, v, *lens, causal=causal)
+    check_prompt(q, k, v, *lens, out, lse, causal=causal)
+
+
+@pytest.mark.parametrize("kind", [BF16, F16])
+@pytest.mark.parametrize("dim", [8, 24, 40, 72, 96, 104, 136, 192, 248])
+def test_prompt_head_dims(ibp, kind, dim):
+    lens = [97, 31], [97, 140]
+    q, k, v = inputs(kind, 2, 1, dim, *lens, seed=dim)
+    out, lse = run_prompt(ibp, q, k, v, *lens)
+    check_prompt(q, k, v, *lens, out, lse)
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(8, 8), (16, 8), (12, 4), (5, 1), (16, 16), (40, 8)])
+def test_prompt_head_groups(ibp, heads, kv_heads):
+    lens = [150, 20], [150, 20]
+    q, k, v = inputs(BF16, heads, kv_heads, 64, *lens, seed=heads)
+    out, lse = run_prompt(ibp, q, k, v, *lens)
+    check_prompt(q, k, v, *lens, out, lse)
+
+
+@pytest.mark.parametrize("kind", [BF16, F16])
+@pytest.mark.parametrize("scale", [0.01, 1.0, 30.0])
+def test_prompt_scales_and_moving_maximum(ibp, kind, scale):
+    """Keys whose scores grow along the sequence, so that the running reference moves in every tile, and
+    scales from nearly uniform weights to one key taking all."""
+    lens = [64], [700]
+    q, k, v = inputs(kind, 2, 1, 64, *lens, seed=3)
+    k = (k.float() * torch.linspace(0.01, 2.0, 700)[:, None, None]).to(kind)
+    out, lse = run_prompt(ibp, q, k, v, *lens, scale=scale)
+    check_prompt(q, k, v, *lens, out, lse, scale=scale)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_prompt_many_sequences(ibp, dim):
+    """More sequences than a wave has lanes, empty ones among them."""
+    q_lens = [(7 * i) % 13 for i in range(150)]
+    k_lens = [n + (i % 3) for i, n in enumerate(q_lens)]
+    q, k, v = inputs(BF16, 2, 2, dim, q_lens, k_lens, seed=5)
+    out, lse = run_prompt(ibp, q, k, v, q_lens, k_lens)
+    check_prompt(q, k, v, q_lens, k_lens, out, lse)
+
+
+@pytest.mark.parametrize("kind", [BF16, F16])
+@pytest.mark.parametrize("dim", [64, 80, 128, 256])
+def test_what_is_not_seen_has_no_effect(ibp, kind, dim):
+    """NaN and infinities in keys and values that a row does not see: later tokens, other sequences, and
+    rows of no sequence. The rows that do see them are as they should be too."""
+    lens = [90, 150], [90, 150]
+    q, k, v = inputs(kind, 2, 1, dim, *lens, seed=7)
+    clean, clean_lse = run_prompt(ibp, q, k, v, *lens)
+    for place in (40, 89, 130, 239):                 # tokens of the first and second sequence
+        for bad in (float("nan"), float("inf"), float("-inf")):
+            k2, v2 = k.clone(), v.clone()
+            v2[place, 0, 1] = bad
+            k2[place, 0, 0] = float("nan") if bad != bad else k2[place, 0, 0]
+            out, lse = run_prompt(ibp, q, k2, v2, *lens)
+            first = 0 if place < 90 else 90
+            last = 90 if place < 90 else 240
+            unseen = torch.ones(240, dtype=torch.bool)
+            unseen[place:last] = False
+            assert torch.isfinite(out[unseen]).all() and torch.isfinite(lse[:, unseen]).all()
+            assert torch.allclose(out[unseen].float(), clean[unseen].float(), rtol=0.02, atol=0.02)
+            assert torch.allclose(lse[:, unseen], clean_lse[:, unseen], rtol=1e-5, atol=1e-5)
+            assert first <= place < last
+            if bad != bad:
+                assert torch.isnan(out[place:last]).all() and torch.isnan(lse[:, place:last]).all()
+            else:
+                assert (out[place:last, :, 1].float() == bad).all()
+                rest = torch.arange(dim) != 1
+                assert torch.allclose(out[place:last][..., rest].float(), clean[place:last][..., rest].float(), rtol=0.02, atol=0.02)
+
+
+def test_scores_of_minus_infinity(ibp):
+    """A key of -inf scores -inf for positive queries: no weight; a row with only such keys gives zeros."""
+    q, k, v = inputs(BF16, 1, 1, 64, [70], [70], seed=1)
+    q[:, :, 0] = 1.0
+    k[:30, :, 0] = NEG
+    out, lse = run_prompt(ibp, q, k, v, [70], [70])
+    assert (lse[0, :30] == NEG).all() and (out[:30] == 0).all()
+    keep_q, keep_k = q[30:], k[30:]
+    o, x, o_tol, x_tol = attend(keep_q[:, 0], keep_k[:, 0], v[30:, 0], 64 ** -0.5, visible(40, 40, True))
+    assert ((out[30:, 0].double() - o).abs() <= o_tol).all() and ((lse[0, 30:].double() - x).abs() <= x_tol).all()
+
+
+def test_prompt_strides(ibp):
+    """Heads and rows in any order: slices of one fused tensor, [head][row] order, an output with gaps."""
+    lens = [77, 60], [77, 60]
+    q, k, v = inputs(BF16, 4, 2, 64, *lens, seed=9)
+    want, want_lse = run_prompt(ibp, q, k, v, *lens)
+    fused = torch.cat([q, k, v], 1).cuda()           # [row][q heads, k heads, v heads][dim]
+    out = torch.full((137, 8, 72), 7.0, dtype=BF16, device="cuda")
+    got, lse = run_prompt(ibp, fused[:, :4], fused[:, 4:6], fused[:, 6:], *lens, out=out[:, 1::2, :64])
+    assert torch.equal(got, want) and torch.equal(lse, want_lse)
+    assert (out[:, ::2] == 7).all() and (out[:, :, 64:] == 7).all()
+    turned = [x.transpose(0, 1).contiguous().cuda().transpose(0, 1) for x in (q, k, v)]
+    got, lse = run_prompt(ibp, *turned, *lens)
+    assert torch.equal(got, want) and torch.equal(lse, want_lse)
+    wide = torch.zeros(137, 2, 200, dtype=BF16, device="cuda")
+    wide[..., 16:80] = k.cuda()
+    got, _ = run_prompt(ibp, q, wide[..., 16:80], v, *lens)
+    assert torch.equal(got, want)
+
+
+def test_prompt_offsets_past_32_bits(ibp):
+    """Rows so far apart that their byte offsets need more than 32 bits."""
+    n, stride = 300, 1 << 23                         # 300 rows x 16 MiB
+    g = torch.Generator().manual_seed(2)
+    q, k, v = (torch.randn(n, 1, 64, generator=g).to(BF16) for _ in range(3))
+    pool = torch.empty((n - 1) * stride + 128, dtype=BF16, device="cuda")
+    far = [torch.as_strided(pool, (n, 1, 64), (stride, 64, 1), 64 * i) for i in range(2)]
+    far[0].copy_(k.cuda())
+    far[1].copy_(v.cuda())
+    want, want_lse = run_prompt(ibp, q, k, v, [n], [n])
+    got, lse = run_prompt(ibp, q, far[0], far[1], [n], [n])
+    assert torch.equal(got, want) and torch.equal(lse, want_lse)
+    far[0].copy_(q.cuda())
+    out, lse = run_prompt(ibp, far[0], k, v, [n], [n], out=far[1])
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+def test_rows_of_no_sequence_are_left_alone(ibp):
+    q, k, v = inputs(BF16, 2, 1, 64, [50], [50], seed=4)
+    out = torch.full((50, 2, 64), 7.0, dtype=BF16, device="cuda")
+    lse = torch.full((2, 50), 7.0, device="cuda")
+    at = torch.tensor([10, 30], dtype=torch.int32, device="cuda")
+    ibp.ibp_attn_prompt(q.cuda(), k.cuda(), v.cuda(), at, at, out, lse)
+    w = torch.full((1, 50), 7.0, device="cuda")
+    ibp.ibp_attn_key_weights(q.cuda(), k.cuda(), at, at, lse, w)
+    for x in (out.transpose(0, 1), lse, w):
+        assert (x[:, :10] == 7).all() and (x[:, 30:] == 7).all() and (x[:, 10:30] != 7).any()
+    check_prompt(q[10:30], k[10:30], v[10:30], [20], [20], out[10:30].cpu(), lse[:, 10:30].cpu())
+
+
+def test_starts_out_of_range_are_clamped(ibp):
+    """Starts are only read on the device: ones beyond the tensors end there, and a falling pair is empty."""
+    q, k, v = inputs(BF16, 1, 1, 64, [40], [40], seed=4)
+    want, want_lse = run_prompt(ibp, q, k, v, [40], [40])
+    out = torch.full((40, 1, 64), 7.0, dtype=BF16, device="cuda")
+    at = torch.tensor([-5, 400, 3], dtype=torch.int32, device="cuda")
+    ibp.ibp_attn_prompt(q.cuda(), k.cuda(), v.cuda(), at, at, out)
+    assert torch.equal(out.cpu(), want)
+
+
+def test_empty_calls(ibp):
+    none = torch.zeros(0, 2, 64, dtype=BF16, device="cuda")
+    at = torch.zeros(1, dtype=torch.int32, device="cuda")
+    ibp.ibp_attn_prompt(none, none, none, at, at, none)
+    ibp.ibp_attn_key_weights(none, none, at, at, torch.zeros(2, 0, device="cuda"), torch.zeros(2, 0, device="cuda"))
+    q = torch.ones(3, 2, 64, dtype=BF16, device="cuda")
+    at, zero = torch.tensor([0, 3], dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    out, lse = torch.full_like(q, 7.0), torch.zeros(2, 3, device="cuda")
+    ibp.ibp_attn_prompt(q, none, none, at, zero, out, lse)
+    assert (out == 0).all() and (lse == NEG).all()
+
+
+def run_weights(ibp, q, k, q_lens, k_lens, lse, causal=True, scale=None):
+    w = torch.full((k.shape[1], k.shape[0]), 7.0, device="cuda")
+    ibp.ibp_attn_key_weights(q.cuda(), k.cuda(), starts(q_lens).cuda(), starts(k_lens).cuda(), lse.cuda(), w, causal=causal,
+                             scale=scale)
+    return w.cpu()
+
+
+def check_weights(q, k, q_lens, k_lens, lse, w, causal=True, scale=None):
+    scale = q.shape[2] ** -0.5 if scale is None else scale
+    group = q.shape[1] // k.shape[1]
+    q0 = k0 = 0
+    for ql, kl in zip(q_lens, k_lens):
+        rq, rk = slice(q0, q0 + ql), slice(k0, k0 + kl)
+        q0, k0 = q0 + ql, k0 + kl
+        for g in range(k.shape[1]):
+            parts = [key_weights(q[rq, h], k[rk, g], lse[h, rq], scale, visible(ql, kl, causal))
+                     for h in range(g * group, (g + 1) * group)]
+            want, tol = sum(p[0] for p in parts), sum(p[1] for p in parts)
+            tol = tol + group * 2.0 ** -24 * want
+            assert ((w[g, rk].double() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("lens", LENGTHS, ids=[f"q{a}-k{b}".replace(" ", "") for a, b in LENGTHS])
+@pytest.mark.parametrize("kind,heads,kv_heads,dim", [(BF16, 4, 2, 128), (F16, 3, 1, 64), (BF16, 2, 2, 80), (F16, 2, 1, 256)])
+def test_key_weights(ibp, kind, heads, kv_heads, dim, lens, causal):
+    q, k, v = inputs(kind, heads, kv_heads, dim, *lens, seed=11)
+    _, lse = run_prompt(ibp, q, k, v, *lens, causal=causal)
+    w = run_weights(ibp, q, k, *lens, lse, causal=causal)
+    check_weights(q, k, *lens, lse, w, causal=causal)
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim", [(8, 8, 40), (16, 2, 96), (7, 7, 136)])
+def test_key_weights_heads_and_dims(ibp, heads, kv_heads, dim):
+    lens = [70, 300], [70, 311]
+    q, k, v = inputs(F16, heads, kv_heads, dim, *lens, seed=13)
+    _, lse = run_prompt(ibp, q, k, v, *lens)
+    check_weights(q, k, *lens, lse, run_weights(ibp, q, k, *lens, lse))
+
+
+def test_key_weights_sum_to_the_rows(ibp):
+    """Every row gives one in all: a sequence's weights sum to rows x query heads."""
+    lens = [1000], [1000]
+    q, k, v = inputs(BF16, 8, 2, 128, *lens, seed=17)
+    _, lse = run_prompt(ibp, q, k, v, *lens)
+    w = run_weights(ibp, q, k, *lens, lse)
+    assert torch.allclose(w.double().sum(1), torch.full((2,), 4000.0, dtype=torch.float64), rtol=1e-5)
+
+
+def test_key_weights_ignore_what_does_not_count(ibp):
+    """A NaN row counts only for the keys it sees, a NaN key only for itself, a row without an lse not at all."""
+    lens = [150], [150]
+    q, k, v = inputs(BF16, 2, 1, 128, *lens, seed=19)
+    _, lse = run_prompt(ibp, q, k, v, *lens)
+    clean = run_weights(ibp, q, k, *lens, lse)
+    q2, lse2 = q.clone(), lse.clone()
+    q2[60], lse2[:, 60] = float("nan"), float("nan")
+    w = run_weights(ibp, q2, k, *lens, lse2)
+    assert torch.isnan(w[:, :61]).all() and torch.equal(w[:, 61:], clean[:, 61:])
+    k2 = k.clone()
+    k2[90] = float("inf")
+    w = run_weights(ibp, q, k2, *lens, lse)
+    other = torch.arange(150) != 90
+    assert torch.equal(w[:, other], clean[:, other])
+    lse2 = lse.clone()
+    lse2[:, 140] = NEG
+    w = run_weights(ibp, q, k, *lens, lse2)
+    check_weights(q, k, *lens, lse2, w)
+
+
+def test_same_result_every_time_and_on_any_stream(ibp):
+    lens = [300, 50], [300, 80]
+    q, k, v = inputs(BF16, 8, 2, 128, *lens, seed=23)
+    out, lse = run_prompt(ibp, q, k, v, *lens)
+    w = run_weights(ibp, q, k, *lens, lse)
+    for _ in range(3):
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            again, again_lse = run_prompt(ibp, q, k, v, *lens)
+            again_w = run_weights(ibp, q, k, *lens, lse)
+        s.synchronize()
+        assert torch.equal(again, out) and torch.equal(again_lse, lse) and torch.equal(again_w, w)
+
+
+def test_binding_refuses(ibp):
+    q, k, v = (x.cuda() for x in inputs(BF16, 2, 1, 64, [8], [8]))
+    at = starts([8]).cuda()
+    out, lse, w = torch.empty_like(q), torch.empty(2, 8, device="cuda"), torch.empty(1, 8, device="cuda")
+    call = lambda **x: ibp.ibp_attn_prompt(*({**dict(q=q, k=k, v=v, a=at, b=at, out=out), **x}[n] for n in  # noqa: E731
+                                             ("q", "k", "v", "a", "b", "out")), x.get("lse"), scale=x.get("scale"))
+    for error, bad in [(TypeError, dict(q=q.cpu())), (TypeError, dict(q=q.float())), (TypeError, dict(k=k.half())),
+                       (ValueError, dict(k=k[:, :, :56])), (ValueError, dict(v=v[0])), (TypeError, dict(a=at.long())),
+                       (ValueError, dict(a=torch.cat([at, at]))), (ValueError, dict(lse=lse[:1])),
+                       (TypeError, dict(out=out.cpu())), (ValueError, dict(out=out[:, :1])),
+                       (TypeError, dict(q=q.transpose(1, 2).contiguous().transpose(1, 2))),
+                       (ibp.IbpError, dict(scale=0.0)), (ibp.IbpError, dict(scale=float("nan"))),
+                       (ibp.IbpError, dict(out=out[:4])), (ibp.IbpError, dict(v=v[:4]))]:
+        with pytest.raises(error):
+            call(**bad)
+    with pytest.raises(ibp.IbpError) as e:           # 16-byte alignment
+        shifted = torch.zeros(8 * 64 + 1, dtype=BF16, device="cuda")[1:].view(8, 1, 64)
+        call(k=shifted)
+    assert e.value.status == ibp.IBP_EINVAL
+    with pytest.raises(ibp.IbpError) as e:
+        ibp.ibp_attn_key_weights(q, k, at, at, lse, w, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    assert e.value.status == ibp.IBP_ENOMEM
