@@ -136,9 +136,9 @@ def _space(workspace, need, device):
     return workspace.data_ptr(), workspace.numel(), workspace
 
 
-def _stream(stream):
-    if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+def _stream(stream, device):
+    if stream is None:       # the current stream's handle, without a Stream object around it
+        return torch._C._cuda_getCurrentRawStream(device)
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -157,7 +157,7 @@ def ibp_attn_prompt(q, k, v, q_starts, k_starts, out, lse=None, causal=True, sca
     n = _starts(q_starts, k_starts, device)
     lse_at = None if lse is None else _array(lse, "lse", torch.float32, device, (heads, q.shape[0]))
     a = _attn(q, kv_heads, dim, scale, causal)
-    check(lib().ibp_attn_prompt(a, rq, rk, rv, q_starts.data_ptr(), k_starts.data_ptr(), n, ro, lse_at, _stream(stream)),
+    check(lib().ibp_attn_prompt(a, rq, rk, rv, q_starts.data_ptr(), k_starts.data_ptr(), n, ro, lse_at, _stream(stream, device)),
           "ibp_attn_prompt")
 
 
@@ -184,7 +184,7 @@ def ibp_attn_key_weights(q, k, q_starts, k_starts, lse, weights, causal=True, sc
     need = ibp_attn_key_weights_workspace(heads, kv_heads, k.shape[0]) if workspace is None else 0
     at, size, held = _space(workspace, need, device)
     check(lib().ibp_attn_key_weights(a, rq, rk, q_starts.data_ptr(), k_starts.data_ptr(), n, lse_at, weights_at, at, size,
-                                     _stream(stream)), "ibp_attn_key_weights")
+                                     _stream(stream, device)), "ibp_attn_key_weights")
 
 
 def ibp_attn_decode_workspace(n_seqs, q_heads, kv_heads, head_dim, max_len, weights):
@@ -222,7 +222,7 @@ def ibp_attn_decode(q, k, v, table, lens, max_len, out, lse=None, weights=None, 
     if workspace is None:
         need = ibp_attn_decode_workspace(n, heads, kv_heads, dim, max_len, weights is not None)
     at, size, held = _space(workspace, need, device)
-    check(lib().ibp_attn_decode(a, rq, pages, lens_at, max_len, ro, lse_at, weights_at, slots, at, size, _stream(stream)),
+    check(lib().ibp_attn_decode(a, rq, pages, lens_at, max_len, ro, lse_at, weights_at, slots, at, size, _stream(stream, device)),
           "ibp_attn_decode")
 
 
@@ -256,4 +256,4 @@ def ibp_kv_evict(k, v, table, lens, max_len, budget, recent, next_positions, wei
     at, size, held = _space(workspace, need, device)
     check(lib().ibp_kv_evict(a, pages, lens_at, n, max_len, budget, recent, next_at, weights_at, positions_at,
                              weights.shape[2], new_weights_at, new_positions_at, new_weights.shape[2], new_lens_at, at,
-                             size, _stream(stream)), "ibp_kv_evict")
+                             size, _stream(stream, device)), "ibp_kv_evict")

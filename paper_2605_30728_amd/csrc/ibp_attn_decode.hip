@@ -40,7 +40,13 @@ __device__ __forceinline__ int slots_of(const DecodeArgs &a, uint32_t seq) {
     return min(max(a.lens[seq], 0), (int)a.max_len);
 }
 
-template <class T, int DIM>
+// What a part with this reference and sum counts for beside the common reference; below zero: it
+// saw no key at all (one that only saw NaN has a reference of -inf too, but a sum of NaN).
+__device__ __forceinline__ float part_of(float ref, float sum, float top, float c) {
+    return ref == -__builtin_inff() ? (sum == 0.f ? -1.f : 1.f) : exp2_fast((ref - top) * c);
+}
+
+template <class T, int DIM, bool FULL>
 __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_decode(DecodeArgs a) {
     constexpr int KS = DIM / 32, DT = DIM / 16, RB = Tile<DIM>::kRowBytes, CH = Tile<DIM>::kChunks;
     constexpr int kChunkBytes = kChunk * RB, VL = kChunkBytes / 1024, kRowsPer = 64 / CH;
@@ -62,23 +68,17 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_decode
     {
         const uint8_t *qp = (const uint8_t *)a.q.data + ((int64_t)seq * a.q.row + (int64_t)(head0 + min(col, heads - 1)) * a.q.head) * 2;
 #pragma unroll
-        for (int x = 0; x < KS; ++x) {
-            const int d = x * 32 + quarter * 8;
-            q[x] = Frag{0, 0, 0, 0};
-            if (d < (int)a.dim) q[x] = *reinterpret_cast<const Frag *>(qp + d * 2);
-        }
+        for (int x = 0; x < KS; ++x) q[x] = load_head<FULL>(qp, x * 32 + quarter * 8, a.dim);
     }
 
+    // lane i < 32 of a wave (and i + 32) knows the page of slot i of a chunk, and its place there
     const int32_t *table = a.pg.table + (int64_t)seq * a.pg.table_stride;
-    // a slot's page and place in it, and whether there is such a page
-    auto find = [&](int slot, int &page, int &place) {
-        const uint32_t s = min(slot, len - 1);
+    int page = 0, place = 0;
+    auto find = [&](int chunk) {
+        const uint32_t s = min(chunk + (lane & 31), len - 1);
         const uint32_t i = a.pg.page_magic ? __umulhi(s, a.pg.page_magic) >> a.pg.page_shift : s >> a.pg.page_shift;
         place = (int)(s - i * a.pg.page_tokens);
-        const int32_t p = table[i];
-        const bool there = slot < len && (uint32_t)p < a.pg.n_pages;
-        page = (uint32_t)p < a.pg.n_pages ? p : 0;
-        return there;
+        page = table[i];
     };
 
     const float inf = __builtin_inff();
@@ -89,37 +89,39 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_decode
     for (int d = 0; d < DT; ++d) acc[d] = f32x4{};
     uint8_t *vt = lds + wave * kWaveBytes;
 
+    constexpr int kStep = kWaves * kChunk;
     Frag kf[2][KS], vf[VL];
     uint64_t live = 0;                   // bit i: slot i of the chunk is there
+    const uint8_t *kbase = (const uint8_t *)a.pg.k.data + (int64_t)kv * a.pg.k.head * 2;
+    const uint8_t *vbase = (const uint8_t *)a.pg.v.data + (int64_t)kv * a.pg.v.head * 2;
+    auto of_slot = [](int64_t x, int slot) {         // lane `slot`'s x
+        return (int64_t)((uint64_t)(uint32_t)__shfl((int)(x >> 32), slot) << 32 | (uint32_t)__shfl((int)x, slot));
+    };
+    // the loads of a chunk whose pages are known, and the look-up of the next one's, so that
+    // nothing waits for a look-up
     auto load = [&](int chunk) {
-        int page, place;
-        const bool there = find(chunk + (lane & 31), page, place);
-        live = __ballot(there) & 0xffffffffull;
+        const bool in = (uint32_t)page < a.pg.n_pages;
+        live = __ballot(in && chunk + (lane & 31) < len) & 0xffffffffull;
+        const int64_t pg = in ? page : 0;
+        const int64_t ko = (pg * a.pg.k.page + (int64_t)place * a.pg.k.token) * 2, vo = (pg * a.pg.v.page + (int64_t)place * a.pg.v.token) * 2;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const int at = j * 16 + col;
-            const uint8_t *kp = (const uint8_t *)a.pg.k.data + ((int64_t)__shfl(page, at) * a.pg.k.page + (int64_t)__shfl(place, at) * a.pg.k.token +
-                                                                (int64_t)kv * a.pg.k.head) * 2;
+            const uint8_t *kp = kbase + of_slot(ko, j * 16 + col);
 #pragma unroll
-            for (int x = 0; x < KS; ++x) {
-                const int d = x * 32 + quarter * 8;
-                kf[j][x] = Frag{0, 0, 0, 0};
-                if (d < (int)a.dim) kf[j][x] = *reinterpret_cast<const Frag *>(kp + d * 2);
-            }
+            for (int x = 0; x < KS; ++x) kf[j][x] = load_head<FULL>(kp, x * 32 + quarter * 8, a.dim);
         }
 #pragma unroll
-        for (int i = 0; i < VL; ++i) {
-            const int row = i * kRowsPer + lane / CH, ch = lane % CH;
-            const uint8_t *vp = (const uint8_t *)a.pg.v.data + ((int64_t)__shfl(page, row) * a.pg.v.page + (int64_t)__shfl(place, row) * a.pg.v.token +
-                                                                (int64_t)kv * a.pg.v.head) * 2;
-            vf[i] = Frag{0, 0, 0, 0};
-            if (ch * 8 < (int)a.dim && (live >> row & 1)) vf[i] = *reinterpret_cast<const Frag *>(vp + ch * 16);
-        }
+        for (int i = 0; i < VL; ++i)
+            vf[i] = load_head<FULL>(vbase + of_slot(vo, i * kRowsPer + lane / CH), lane % CH * 8, a.dim);
+        find(chunk + kStep);
     };
 
     int chunk = from + wave * kChunk;
-    if (chunk < to) load(chunk);
-    for (; chunk < to; chunk += kWaves * kChunk) {
+    if (chunk < to) {
+        find(chunk);
+        load(chunk);
+    }
+    for (; chunk < to; chunk += kStep) {
         f32x4 s[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -127,21 +129,25 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_decode
 #pragma unroll
             for (int x = 0; x < KS; ++x) s[j] = T::mfma16(kf[j][x], q[x], s[j]);
         }
-#pragma unroll
-        for (int i = 0; i < VL; ++i) {
-            const int row = i * kRowsPer + lane / CH, ch = lane % CH;
-            *reinterpret_cast<Frag *>(vt + row * RB + ((ch ^ Tile<DIM>::columns(row)) << 4)) = vf[i];
-        }
         const uint64_t now = live;
-        if (chunk + kWaves * kChunk < to) load(chunk + kWaves * kChunk);
-
-        if (now != 0xffffffffull) {
+        if (now != 0xffffffffull) {      // slots that are not there: no score, and no value that a weight of 0 could meet
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     if (!(now >> (j * 16 + quarter * 4 + i) & 1)) s[j][i] = -inf;
+#pragma unroll
+            for (int i = 0; i < VL; ++i) {
+                const bool in = now >> (i * kRowsPer + lane / CH) & 1;
+                vf[i] = Frag{in ? vf[i][0] : 0, in ? vf[i][1] : 0, in ? vf[i][2] : 0, in ? vf[i][3] : 0};
+            }
         }
+#pragma unroll
+        for (int i = 0; i < VL; ++i) {
+            const int row = i * kRowsPer + lane / CH, ch = lane % CH;
+            *reinterpret_cast<Frag *>(vt + row * RB + ((ch ^ Tile<DIM>::columns(row)) << 4)) = vf[i];
+        }
+        if (chunk + kStep < to) load(chunk + kStep);
         if (a.scores && col < heads) {
             float *sp = a.scores + ((int64_t)seq * a.q_heads + head0 + col) * a.scores_stride + chunk + quarter * 4;
 #pragma unroll
@@ -197,8 +203,8 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_decode
     float part[kWaves];
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-        part[w] = stat[w][0][h] == -inf ? (stat[w][1][h] == 0.f ? 0.f : 1.f) : exp2_fast((stat[w][0][h] - top) * c);
-        sum += part[w] * stat[w][1][h];
+        part[w] = part_of(stat[w][0][h], stat[w][1][h], top, c);
+        if (!(part[w] < 0.f)) sum += part[w] * stat[w][1][h];
     }
     const uint32_t head = head0 + h;
     const bool last = a.splits == 1;
@@ -207,7 +213,7 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_decode
         f32x4 x{};
 #pragma unroll
         for (int w = 0; w < kWaves; ++w)
-            if (part[w] != 0.f) x += part[w] * *reinterpret_cast<const f32x4 *>(reinterpret_cast<float *>(lds + w * kWaveBytes) + h * (DIM + 4) + d);
+            if (!(part[w] < 0.f)) x += part[w] * *reinterpret_cast<const f32x4 *>(reinterpret_cast<float *>(lds + w * kWaveBytes) + h * (DIM + 4) + d);
         x *= inv;
         if (last) {
             u32x2 o;
@@ -228,81 +234,117 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_decode
     }
 }
 
-// The splits of a sequence that a head has, and their joint reference and sum.
-__device__ __forceinline__ void join_stats(const DecodeArgs &a, uint32_t seq, uint32_t head, uint32_t n, float &top, float &sum) {
-    const int lane = threadIdx.x & 63;
-    const float *st = a.stats + ((int64_t)seq * a.q_heads + head) * a.splits * 2;
-    const float inf = __builtin_inff();
-    top = -inf;
-    for (uint32_t x = lane; x < n; x += 64) top = fmaxf(top, st[x * 2]);
-    for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
-    sum = 0.f;
-    for (uint32_t x = lane; x < n; x += 64)
-        sum += st[x * 2] == -inf ? st[x * 2 + 1] : st[x * 2 + 1] * exp2_fast((st[x * 2] - top) * a.scale_log2);
-    for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x);
+constexpr int kJoinThreads = 256;
+constexpr int kJoinSlots = 4 * kJoinThreads; // slots whose weights a block of the second kernel adds
+constexpr uint32_t kMaxSplits = 1024;
+
+// x over the block's threads, by `op` with neutral element `none`.
+template <class Op>
+__device__ __forceinline__ float block_reduce(float x, float none, float *waves, Op op) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) x = op(x, __shfl_xor(x, d));
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = none;
+#pragma unroll
+    for (int w = 0; w < kJoinThreads / 64; ++w) x = op(x, waves[w]);
+    return x;
 }
 
-constexpr int kJoinSlots = 1024;             // slots whose weights a block of the second kernel adds
-
-// Block 0 of a (sequence, KV head) joins the splits of its query heads, a wave each in turn; the
-// others add the weights of kJoinSlots slots.
+// Of the blocks of a (sequence, KV head), one for each query head joins that head's splits (where
+// there are several); the others add the weights of kJoinSlots slots.
 template <class T>
-__global__ __launch_bounds__(256) void k_attn_decode_join(DecodeArgs a, uint32_t weight_blocks) {
-    const uint32_t per = weight_blocks + (a.splits > 1 ? 1 : 0);
+__global__ __launch_bounds__(kJoinThreads) void k_attn_decode_join(DecodeArgs a, uint32_t weight_blocks) {
+    __shared__ float part[kMaxSplits];
+    __shared__ f32x4 sums[kJoinThreads];
+    __shared__ float waves[kJoinThreads / 64];
+    const uint32_t per = weight_blocks + (a.splits > 1 ? a.group : 0);
     const uint32_t x = blockIdx.x % per, kv = blockIdx.x / per % a.kv_heads, seq = blockIdx.x / per / a.kv_heads;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int len = slots_of(a, seq);
-    const uint32_t n = len > 0 ? (len + a.split_tokens - 1) / a.split_tokens : 1;
-    const float inf = __builtin_inff();
-    if (x == weight_blocks) {
-        for (uint32_t g = wave; g < a.group; g += 4) {
-            const uint32_t head = kv * a.group + g;
-            float top, sum;
-            join_stats(a, seq, head, n, top, sum);
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
-            const float *st = a.stats + ((int64_t)seq * a.q_heads + head) * a.splits * 2;
-            const float *pp = a.partial + ((int64_t)seq * a.q_heads + head) * a.splits * a.dim;
-            for (int d = lane * 2; d < (int)a.dim; d += 128) {
-                f32x2 o{};
-                for (uint32_t y = 0; y < n; ++y) {
-                    if (st[y * 2 + 1] == 0.f) continue;
-                    const float f = st[y * 2] == -inf ? 1.f : exp2_fast((st[y * 2] - top) * a.scale_log2);
-                    o += f * *reinterpret_cast<const f32x2 *>(pp + (int64_t)y * a.dim + d);
-                }
-                *reinterpret_cast<uint32_t *>((uint8_t *)a.out.data + ((int64_t)seq * a.out.row + (int64_t)head * a.out.head + d) * 2) =
-                    T::pack(o[0] * inv, o[1] * inv);
-            }
-            if (a.lse && lane == 0) a.lse[(int64_t)seq * a.q_heads + head] = sum == 0.f ? -inf : top * a.scale + __logf(sum);
+    const int n = len > 0 ? (int)((len + a.split_tokens - 1) / a.split_tokens) : 1;
+    const float inf = __builtin_inff(), c = a.scale_log2;
+    if (x >= weight_blocks) {
+        const uint32_t head = kv * a.group + x - weight_blocks;
+        const int64_t at = ((int64_t)seq * a.q_heads + head) * a.splits;
+        const f32x2 *st = reinterpret_cast<const f32x2 *>(a.stats) + at;
+        float top = -inf, sum = 0.f;
+        for (int y = threadIdx.x; y < n; y += kJoinThreads) top = fmaxf(top, st[y][0]);
+        top = block_reduce(top, -inf, waves, [](float u, float v) { return fmaxf(u, v); });
+        for (int y = threadIdx.x; y < n; y += kJoinThreads) {
+            const f32x2 s = st[y];
+            part[y] = part_of(s[0], s[1], top, c);
+            if (!(part[y] < 0.f)) sum += part[y] * s[1];
         }
+        sum = block_reduce(sum, 0.f, waves, [](float u, float v) { return u + v; });
+        // four dims per thread, the splits shared out over the groups of threads that hold all dims
+        const int quads = a.dim / 4, groups = kJoinThreads / quads, d = threadIdx.x % quads, y0 = threadIdx.x / quads;
+        const f32x4 *pp = reinterpret_cast<const f32x4 *>(a.partial + at * a.dim);
+        f32x4 o{};
+        if (y0 < groups)
+            for (int y = y0; y < n; y += groups)
+                if (!(part[y] < 0.f)) o += part[y] * pp[(int64_t)y * quads + d];
+        sums[threadIdx.x] = o;
+        __syncthreads();
+        if (y0 != 0) return;
+        for (int y = 1; y < groups; ++y) o += sums[y * quads + d];
+        o *= sum == 0.f ? 0.f : 1.f / sum;
+        u32x2 w;
+        w[0] = T::pack(o[0], o[1]);
+        w[1] = T::pack(o[2], o[3]);
+        *reinterpret_cast<u32x2 *>((uint8_t *)a.out.data + ((int64_t)seq * a.out.row + (int64_t)head * a.out.head + d * 4) * 2) = w;
+        if (a.lse && d == 0) a.lse[(int64_t)seq * a.q_heads + head] = sum == 0.f ? -inf : top * a.scale + __logf(sum);
         return;
     }
-    const int slot0 = x * kJoinSlots + threadIdx.x * 4;
     if ((int)(x * kJoinSlots) >= len) return;
+    const int lane = threadIdx.x & 63, slot = x * kJoinSlots + threadIdx.x * 4;
     float w[4] = {};
-    for (uint32_t g = 0; g < a.group; ++g) {
-        const uint32_t head = kv * a.group + g;
-        float top, sum;
-        join_stats(a, seq, head, n, top, sum);
-        const float inv = sum == 0.f ? 0.f : 1.f / sum, mc = top == -inf ? 0.f : top * a.scale_log2;
-        if (slot0 < len) {
-            const f32x4 s = *reinterpret_cast<const f32x4 *>(a.scores + ((int64_t)seq * a.q_heads + head) * a.scores_stride + slot0);
+    for (uint32_t g0 = 0; g0 < a.group; g0 += 64) {          // (64 heads' references and sums at a time)
+        const int heads = min((int)(a.group - g0), 64);
+        __syncthreads();
+        for (int h = threadIdx.x >> 6; h < heads; h += kJoinThreads / 64) {
+            const f32x2 *st = reinterpret_cast<const f32x2 *>(a.stats) + ((int64_t)seq * a.q_heads + kv * a.group + g0 + h) * a.splits;
+            float top = -inf, sum = 0.f;
+            for (int y = lane; y < n; y += 64) top = fmaxf(top, st[y][0]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] += exp2_fast(__builtin_fmaf(s[i], a.scale_log2, -mc)) * inv;
+            for (int y = 1; y < 64; y <<= 1) top = fmaxf(top, __shfl_xor(top, y));
+            for (int y = lane; y < n; y += 64) {
+                const f32x2 s = st[y];
+                const float f = part_of(s[0], s[1], top, c);
+                if (!(f < 0.f)) sum += f * s[1];
+            }
+#pragma unroll
+            for (int y = 1; y < 64; y <<= 1) sum += __shfl_xor(sum, y);
+            if (lane == 0) {
+                part[h * 2] = top == -inf ? 0.f : top * c;
+                part[h * 2 + 1] = sum == 0.f ? 0.f : 1.f / sum;
+            }
+        }
+        __syncthreads();
+        if (slot >= len) continue;
+        const float *sp = a.scores + ((int64_t)seq * a.q_heads + kv * a.group + g0) * a.scores_stride + slot;
+#pragma unroll 4
+        for (int h = 0; h < heads; ++h) {
+            const f32x4 s = *reinterpret_cast<const f32x4 *>(sp + (int64_t)h * a.scores_stride);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] += exp2_fast(__builtin_fmaf(s[i], c, -part[h * 2])) * part[h * 2 + 1];
         }
     }
-    float *out = a.weights + ((int64_t)seq * a.kv_heads + kv) * a.weights_stride + slot0;
+    float *out = a.weights + ((int64_t)seq * a.kv_heads + kv) * a.weights_stride + slot;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        if (slot0 + i < len) out[i] += w[i];
+        if (slot + i < len) out[i] += w[i];
 }
 
 template <class T>
 void decode_of(const DecodeArgs &a, uint32_t blocks, hipStream_t stream) {
     const dim3 grid(blocks), block(64 * kWaves);
-    if (a.dim <= 64) k_attn_decode<T, 64><<<grid, block, 0, stream>>>(a);
-    else if (a.dim <= 96) k_attn_decode<T, 96><<<grid, block, 0, stream>>>(a);
-    else if (a.dim <= 128) k_attn_decode<T, 128><<<grid, block, 0, stream>>>(a);
-    else k_attn_decode<T, 256><<<grid, block, 0, stream>>>(a);
+    if (a.dim == 64) k_attn_decode<T, 64, true><<<grid, block, 0, stream>>>(a);
+    else if (a.dim < 64) k_attn_decode<T, 64, false><<<grid, block, 0, stream>>>(a);
+    else if (a.dim < 128) k_attn_decode<T, 128, false><<<grid, block, 0, stream>>>(a);
+    else if (a.dim == 128) k_attn_decode<T, 128, true><<<grid, block, 0, stream>>>(a);
+    else if (a.dim < 256) k_attn_decode<T, 256, false><<<grid, block, 0, stream>>>(a);
+    else k_attn_decode<T, 256, true><<<grid, block, 0, stream>>>(a);
 }
 
 uint64_t up256(uint64_t x) { return (x + 255) / 256 * 256; }
@@ -313,13 +355,15 @@ DecodePlan plan_decode(uint32_t n_seqs, uint32_t q_heads, uint32_t kv_heads, uin
                        bool weights) {
     DecodePlan p{};
     p.head_blocks = (q_heads / kv_heads + 15) / 16;
-    // enough blocks to fill the chip, of at least 128 slots (one chunk per wave)
-    const uint64_t rows = std::max<uint64_t>((uint64_t)n_seqs * kv_heads * p.head_blocks, 1);
-    const uint64_t want = (1024 + rows - 1) / rows;
-    uint64_t t = (std::max<uint64_t>(max_len, 1) + want - 1) / want;
+    // two blocks of one CU each for a single sequence; of several, whose lengths differ, blocks of
+    // 1,024 slots that even out; at least 128 slots (a chunk per wave)
+    const uint64_t rows = std::max<uint64_t>((uint64_t)n_seqs * kv_heads * p.head_blocks, 1), len = std::max<uint64_t>(max_len, 1);
+    uint64_t t = (len * rows + 511) / 512;
+    if (n_seqs > 1) t = std::min<uint64_t>(t, 1024);
+    t = std::max<uint64_t>(t, (len + kMaxSplits - 1) / kMaxSplits);
     t = std::max<uint64_t>((t + 127) / 128 * 128, 128);
     p.split_tokens = (uint32_t)t;
-    p.splits = (uint32_t)((std::max<uint64_t>(max_len, 1) + t - 1) / t);
+    p.splits = (uint32_t)((len + t - 1) / t);
     const uint64_t parts = (uint64_t)n_seqs * q_heads * p.splits;
     p.stats_off = 0;
     p.out_off = up256(parts * 8);
@@ -334,7 +378,7 @@ hipError_t launch_decode(const Shape &s, const Rows &q, const Pages &pg, const i
     if (n_seqs == 0) return hipSuccess;
     const uint64_t blocks = (uint64_t)n_seqs * plan.splits * s.kv_heads * plan.head_blocks;
     const uint32_t weight_blocks = weights ? (max_len + kJoinSlots - 1) / kJoinSlots : 0;
-    const uint64_t join = (uint64_t)n_seqs * s.kv_heads * (weight_blocks + (plan.splits > 1 ? 1 : 0));
+    const uint64_t join = (uint64_t)n_seqs * s.kv_heads * (weight_blocks + (plan.splits > 1 ? s.group : 0));
     if (blocks > kMaxGrid || join > kMaxGrid) return hipErrorInvalidConfiguration;
     DecodeArgs a{q, out, pg, lens, lse, weights, weights_stride, (float *)(workspace + plan.stats_off),
                  (float *)(workspace + plan.out_off), weights ? (float *)(workspace + plan.scores_off) : nullptr,
@@ -343,8 +387,8 @@ hipError_t launch_decode(const Shape &s, const Rows &q, const Pages &pg, const i
     if (s.f16) decode_of<F16>(a, (uint32_t)blocks, stream);
     else decode_of<Bf16>(a, (uint32_t)blocks, stream);
     if (join) {
-        if (s.f16) k_attn_decode_join<F16><<<dim3((uint32_t)join), dim3(256), 0, stream>>>(a, weight_blocks);
-        else k_attn_decode_join<Bf16><<<dim3((uint32_t)join), dim3(256), 0, stream>>>(a, weight_blocks);
+        if (s.f16) k_attn_decode_join<F16><<<dim3((uint32_t)join), dim3(kJoinThreads), 0, stream>>>(a, weight_blocks);
+        else k_attn_decode_join<Bf16><<<dim3((uint32_t)join), dim3(kJoinThreads), 0, stream>>>(a, weight_blocks);
     }
     return hipGetLastError();
 }

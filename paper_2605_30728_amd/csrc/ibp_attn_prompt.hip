@@ -138,11 +138,7 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_prompt
     {
         const uint8_t *qp = (const uint8_t *)a.q.data + ((int64_t)(st.q0 + seen_row) * a.q.row + (int64_t)head * a.q.head) * 2;
 #pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            const int d = s * 16 + half * 8;
-            q[s] = Frag{0, 0, 0, 0};
-            if (d < (int)a.dim) q[s] = *reinterpret_cast<const Frag *>(qp + d * 2);
-        }
+        for (int s = 0; s < KS; ++s) q[s] = load_head<false>(qp, s * 16 + half * 8, a.dim);
     }
 
     const float inf = __builtin_inff();

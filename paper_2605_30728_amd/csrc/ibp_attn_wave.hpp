@@ -166,6 +166,16 @@ __device__ __forceinline__ bool has_nonfinite(Frag f) {
     return bad;
 }
 
+// Eight values from place d of a head on; zeros where the head (of `dim` values, a multiple of 8)
+// ends before that. Nothing beyond the head is read. FULL: it never does.
+template <bool FULL>
+__device__ __forceinline__ Frag load_head(const uint8_t *head, int d, int dim) {
+    if constexpr (FULL) return *reinterpret_cast<const Frag *>(head + d * 2);
+    const Frag f = *reinterpret_cast<const Frag *>(head + min(d, dim - 8) * 2);
+    const bool in = d < dim;
+    return Frag{in ? f[0] : 0, in ? f[1] : 0, in ? f[2] : 0, in ? f[3] : 0};
+}
+
 // The sequence and tile of block `t` where a packed sequence of n rows makes ceil(n / tile_rows)
 // tiles: every wave scans the starts, 64 sequences at a time. False: no such tile.
 struct SeqTile {

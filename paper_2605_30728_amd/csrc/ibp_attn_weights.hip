@@ -61,11 +61,7 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_key_we
         const int key = min(key0 + j * 32 + col, k_len - 1);
         const uint8_t *kp = (const uint8_t *)a.k.data + ((int64_t)(st.k0 + key) * a.k.row + (int64_t)kv * a.k.head) * 2;
 #pragma unroll
-        for (int x = 0; x < KS; ++x) {
-            const int d = x * 16 + half * 8;
-            k[j][x] = Frag{0, 0, 0, 0};
-            if (d < (int)a.dim) k[j][x] = *reinterpret_cast<const Frag *>(kp + d * 2);
-        }
+        for (int x = 0; x < KS; ++x) k[j][x] = load_head<false>(kp, x * 16 + half * 8, a.dim);
     }
 
     const uint32_t q_stride = (uint32_t)a.q.row * 2;
