@@ -34,7 +34,11 @@ struct DecodeArgs {
 };
 
 constexpr int kWaves = 4;
-constexpr int kChunk = 32;
+
+// Slots that a wave takes at a time: what its registers hold of K and V while they are on their
+// way, with two waves per SIMD.
+template <int DIM>
+constexpr int chunk_slots() { return DIM <= 128 ? 32 : 16; }
 
 __device__ __forceinline__ int slots_of(const DecodeArgs &a, uint32_t seq) {
     return min(max(a.lens[seq], 0), (int)a.max_len);
@@ -47,7 +51,9 @@ __device__ __forceinline__ float part_of(float ref, float sum, float top, float 
 }
 
 template <class T, int DIM, bool FULL>
-__global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_decode(DecodeArgs a) {
+__global__ __launch_bounds__(64 * kWaves, 2) void k_attn_decode(DecodeArgs a) {
+    constexpr int kChunk = chunk_slots<DIM>(), KT = kChunk / 16;
+    constexpr uint64_t kAll = (1ull << kChunk) - 1;
     constexpr int KS = DIM / 32, DT = DIM / 16, RB = Tile<DIM>::kRowBytes, CH = Tile<DIM>::kChunks;
     constexpr int kChunkBytes = kChunk * RB, VL = kChunkBytes / 1024, kRowsPer = 64 / CH;
     constexpr int kJoin = 16 * (DIM + 4) * 4;        // a wave's sums, for the join
@@ -57,7 +63,9 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_decode
 
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), quarter = lane >> 4, col = lane & 15;
     const uint32_t hb = blockIdx.x % (a.kv_heads * a.head_blocks), rest = blockIdx.x / (a.kv_heads * a.head_blocks);
-    const uint32_t split = rest % a.splits, seq = rest / a.splits;
+    // (splits outermost: those that no sequence reaches come last; and sequences turned by one from split
+    // to split, so that each one's splits run on all XCDs)
+    const uint32_t split = rest / a.n_seqs, seq = (rest % a.n_seqs + split) % a.n_seqs;
     const uint32_t kv = hb / a.head_blocks, head0 = kv * a.group + hb % a.head_blocks * 16;
     const int heads = min((int)((kv + 1) * a.group - head0), 16);
     const int len = uniform(slots_of(a, seq));
@@ -71,11 +79,11 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_decode
         for (int x = 0; x < KS; ++x) q[x] = load_head<FULL>(qp, x * 32 + quarter * 8, a.dim);
     }
 
-    // lane i < 32 of a wave (and i + 32) knows the page of slot i of a chunk, and its place there
+    // lane i < kChunk of a wave (and i + kChunk ...) knows the page of slot i of a chunk, and its place there
     const int32_t *table = a.pg.table + (int64_t)seq * a.pg.table_stride;
     int page = 0, place = 0;
     auto find = [&](int chunk) {
-        const uint32_t s = min(chunk + (lane & 31), len - 1);
+        const uint32_t s = min(chunk + (lane & (kChunk - 1)), len - 1);
         const uint32_t i = a.pg.page_magic ? __umulhi(s, a.pg.page_magic) >> a.pg.page_shift : s >> a.pg.page_shift;
         place = (int)(s - i * a.pg.page_tokens);
         page = table[i];
@@ -90,7 +98,7 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_decode
     uint8_t *vt = lds + wave * kWaveBytes;
 
     constexpr int kStep = kWaves * kChunk;
-    Frag kf[2][KS], vf[VL];
+    Frag kf[KT][KS], vf[VL];
     uint64_t live = 0;                   // bit i: slot i of the chunk is there
     const uint8_t *kbase = (const uint8_t *)a.pg.k.data + (int64_t)kv * a.pg.k.head * 2;
     const uint8_t *vbase = (const uint8_t *)a.pg.v.data + (int64_t)kv * a.pg.v.head * 2;
@@ -101,11 +109,11 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_decode
     // nothing waits for a look-up
     auto load = [&](int chunk) {
         const bool in = (uint32_t)page < a.pg.n_pages;
-        live = __ballot(in && chunk + (lane & 31) < len) & 0xffffffffull;
+        live = __ballot(in && chunk + (lane & (kChunk - 1)) < len) & kAll;
         const int64_t pg = in ? page : 0;
         const int64_t ko = (pg * a.pg.k.page + (int64_t)place * a.pg.k.token) * 2, vo = (pg * a.pg.v.page + (int64_t)place * a.pg.v.token) * 2;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < KT; ++j) {
             const uint8_t *kp = kbase + of_slot(ko, j * 16 + col);
 #pragma unroll
             for (int x = 0; x < KS; ++x) kf[j][x] = load_head<FULL>(kp, x * 32 + quarter * 8, a.dim);
@@ -122,17 +130,17 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_decode
         load(chunk);
     }
     for (; chunk < to; chunk += kStep) {
-        f32x4 s[2];
+        f32x4 s[KT];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < KT; ++j) {
             s[j] = f32x4{};
 #pragma unroll
             for (int x = 0; x < KS; ++x) s[j] = T::mfma16(kf[j][x], q[x], s[j]);
         }
         const uint64_t now = live;
-        if (now != 0xffffffffull) {      // slots that are not there: no score, and no value that a weight of 0 could meet
+        if (now != kAll) {      // slots that are not there: no score, and no value that a weight of 0 could meet
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < KT; ++j)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     if (!(now >> (j * 16 + quarter * 4 + i) & 1)) s[j][i] = -inf;
@@ -151,10 +159,13 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_decode
         if (a.scores && col < heads) {
             float *sp = a.scores + ((int64_t)seq * a.q_heads + head0 + col) * a.scores_stride + chunk + quarter * 4;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) *reinterpret_cast<f32x4 *>(sp + j * 16) = s[j];
+            for (int j = 0; j < KT; ++j) *reinterpret_cast<f32x4 *>(sp + j * 16) = s[j];
         }
-        float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
-                          fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+        float top = s[0][0];
+#pragma unroll
+        for (int j = 0; j < KT; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = fmaxf(top, s[j][i]);
         top = max_halves(max_quarters(top));
         if (__any(top > m)) {
             const float next = fmaxf(m, top);
@@ -165,22 +176,27 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_decode
             m = next;
         }
         const float mc = m == -inf ? 0.f : m * c;
-        Frag p;
+        u32x2 p[KT];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < KT; ++j) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 s[j][i] = exp2_fast(__builtin_fmaf(s[j][i], c, -mc));
                 l += s[j][i];
             }
-            p[j * 2] = T::pack(s[j][0], s[j][1]);
-            p[j * 2 + 1] = T::pack(s[j][2], s[j][3]);
+            p[j][0] = T::pack(s[j][0], s[j][1]);
+            p[j][1] = T::pack(s[j][2], s[j][3]);
         }
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
             const int key = quarter * 4 + (col >> 2), at = d * 16 + (col & 3) * 4;
-            const u32x2 lo = read_columns<DIM>(vt, key, at), hi = read_columns<DIM>(vt, key + 16, at);
-            acc[d] = T::mfma16(Frag{lo[0], lo[1], hi[0], hi[1]}, p, acc[d]);
+            const u32x2 lo = read_columns<DIM>(vt, key, at);
+            if constexpr (KT == 1) {
+                acc[d] = T::mfma16(lo, p[0], acc[d]);
+            } else {
+                const u32x2 hi = read_columns<DIM>(vt, key + 16, at);
+                acc[d] = T::mfma16(Frag{lo[0], lo[1], hi[0], hi[1]}, Frag{p[0][0], p[0][1], p[1][0], p[1][1]}, acc[d]);
+            }
         }
     }
 
@@ -236,6 +252,12 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_decode
 
 constexpr int kJoinThreads = 256;
 constexpr int kJoinSlots = 4 * kJoinThreads; // slots whose weights a block of the second kernel adds
+
+// Dims that a block of the second kernel joins: the whole head where it has few splits (64
+// sequences of 8 heads, 11 splits: 18 us, in blocks of 64 dims 31), 64 where the way through them is long
+// (512 splits of 256 dims: 16 rounds of its threads instead of 128).
+inline uint32_t join_dims(uint32_t dim, uint32_t splits) { return splits > 64 ? std::min(dim, 64u) : dim; }
+
 constexpr uint32_t kMaxSplits = 1024;
 
 // x over the block's threads, by `op` with neutral element `none`.
@@ -252,20 +274,20 @@ __device__ __forceinline__ float block_reduce(float x, float none, float *waves,
     return x;
 }
 
-// Of the blocks of a (sequence, KV head), one for each query head joins that head's splits (where
-// there are several); the others add the weights of kJoinSlots slots.
+// Of the blocks of a (sequence, KV head), one for each query head and join_dims dims joins that
+// head's splits (where there are several); the others add the weights of kJoinSlots slots.
 template <class T>
-__global__ __launch_bounds__(kJoinThreads) void k_attn_decode_join(DecodeArgs a, uint32_t weight_blocks) {
+__global__ __launch_bounds__(kJoinThreads) void k_attn_decode_join(DecodeArgs a, uint32_t weight_blocks, uint32_t dims) {
     __shared__ float part[kMaxSplits];
     __shared__ f32x4 sums[kJoinThreads];
     __shared__ float waves[kJoinThreads / 64];
-    const uint32_t per = weight_blocks + (a.splits > 1 ? a.group : 0);
+    const uint32_t dim_blocks = (a.dim + dims - 1) / dims, per = weight_blocks + (a.splits > 1 ? a.group * dim_blocks : 0);
     const uint32_t x = blockIdx.x % per, kv = blockIdx.x / per % a.kv_heads, seq = blockIdx.x / per / a.kv_heads;
     const int len = slots_of(a, seq);
     const int n = len > 0 ? (int)((len + a.split_tokens - 1) / a.split_tokens) : 1;
     const float inf = __builtin_inff(), c = a.scale_log2;
     if (x >= weight_blocks) {
-        const uint32_t head = kv * a.group + x - weight_blocks;
+        const uint32_t head = kv * a.group + (x - weight_blocks) / dim_blocks, d0 = (x - weight_blocks) % dim_blocks * dims;
         const int64_t at = ((int64_t)seq * a.q_heads + head) * a.splits;
         const f32x2 *st = reinterpret_cast<const f32x2 *>(a.stats) + at;
         float top = -inf, sum = 0.f;
@@ -278,21 +300,26 @@ __global__ __launch_bounds__(kJoinThreads) void k_attn_decode_join(DecodeArgs a,
         }
         sum = block_reduce(sum, 0.f, waves, [](float u, float v) { return u + v; });
         // four dims per thread, the splits shared out over the groups of threads that hold all dims
-        const int quads = a.dim / 4, groups = kJoinThreads / quads, d = threadIdx.x % quads, y0 = threadIdx.x / quads;
-        const f32x4 *pp = reinterpret_cast<const f32x4 *>(a.partial + at * a.dim);
+        const int quads = dims / 4, groups = kJoinThreads / quads;
+        const int q = threadIdx.x % quads, y0 = threadIdx.x / quads, d = d0 + q * 4;
+        const float *pp = a.partial + at * a.dim + d;
         f32x4 o{};
-        if (y0 < groups)
-            for (int y = y0; y < n; y += groups)
-                if (!(part[y] < 0.f)) o += part[y] * pp[(int64_t)y * quads + d];
+        if (d < (int)a.dim && y0 < groups) {
+#pragma unroll 4
+            for (int y = y0; y < n; y += groups) {
+                const f32x4 v = *reinterpret_cast<const f32x4 *>(pp + (int64_t)y * a.dim);
+                if (!(part[y] < 0.f)) o += part[y] * v;
+            }
+        }
         sums[threadIdx.x] = o;
         __syncthreads();
-        if (y0 != 0) return;
-        for (int y = 1; y < groups; ++y) o += sums[y * quads + d];
+        if (y0 != 0 || d >= (int)a.dim) return;
+        for (int y = 1; y < groups; ++y) o += sums[y * quads + q];
         o *= sum == 0.f ? 0.f : 1.f / sum;
         u32x2 w;
         w[0] = T::pack(o[0], o[1]);
         w[1] = T::pack(o[2], o[3]);
-        *reinterpret_cast<u32x2 *>((uint8_t *)a.out.data + ((int64_t)seq * a.out.row + (int64_t)head * a.out.head + d * 4) * 2) = w;
+        *reinterpret_cast<u32x2 *>((uint8_t *)a.out.data + ((int64_t)seq * a.out.row + (int64_t)head * a.out.head + d) * 2) = w;
         if (a.lse && d == 0) a.lse[(int64_t)seq * a.q_heads + head] = sum == 0.f ? -inf : top * a.scale + __logf(sum);
         return;
     }
@@ -355,11 +382,13 @@ DecodePlan plan_decode(uint32_t n_seqs, uint32_t q_heads, uint32_t kv_heads, uin
                        bool weights) {
     DecodePlan p{};
     p.head_blocks = (q_heads / kv_heads + 15) / 16;
-    // two blocks of one CU each for a single sequence; of several, whose lengths differ, blocks of
-    // 1,024 slots that even out; at least 128 slots (a chunk per wave)
+    // a single sequence: the 512 blocks that the chip holds at once (131,071 slots of 8 heads of
+    // 128: 99 us, with 1,024 blocks 103, with 2,048 109). Several, whose lengths differ: up to 1,024
+    // blocks (24 sequences of up to 6,000 slots of one head of 256: 27 us, with 512 31), and more of
+    // 768 slots (64 sequences of up to 8,192 slots: blocks of 4,096 slots 294 us, of 768 to 1,024 259,
+    // of 256 267). At least 128 slots, a chunk or two per wave.
     const uint64_t rows = std::max<uint64_t>((uint64_t)n_seqs * kv_heads * p.head_blocks, 1), len = std::max<uint64_t>(max_len, 1);
-    uint64_t t = (len * rows + 511) / 512;
-    if (n_seqs > 1) t = std::min<uint64_t>(t, 1024);
+    uint64_t t = n_seqs > 1 ? std::min<uint64_t>((len * rows + 1023) / 1024, 768) : (len * rows + 511) / 512;
     t = std::max<uint64_t>(t, (len + kMaxSplits - 1) / kMaxSplits);
     t = std::max<uint64_t>((t + 127) / 128 * 128, 128);
     p.split_tokens = (uint32_t)t;
@@ -378,7 +407,8 @@ hipError_t launch_decode(const Shape &s, const Rows &q, const Pages &pg, const i
     if (n_seqs == 0) return hipSuccess;
     const uint64_t blocks = (uint64_t)n_seqs * plan.splits * s.kv_heads * plan.head_blocks;
     const uint32_t weight_blocks = weights ? (max_len + kJoinSlots - 1) / kJoinSlots : 0;
-    const uint64_t join = (uint64_t)n_seqs * s.kv_heads * (weight_blocks + (plan.splits > 1 ? s.group : 0));
+    const uint32_t dims = join_dims(s.dim, plan.splits), dim_blocks = (s.dim + dims - 1) / dims;
+    const uint64_t join = (uint64_t)n_seqs * s.kv_heads * (weight_blocks + (plan.splits > 1 ? s.group * dim_blocks : 0));
     if (blocks > kMaxGrid || join > kMaxGrid) return hipErrorInvalidConfiguration;
     DecodeArgs a{q, out, pg, lens, lse, weights, weights_stride, (float *)(workspace + plan.stats_off),
                  (float *)(workspace + plan.out_off), weights ? (float *)(workspace + plan.scores_off) : nullptr,
@@ -387,8 +417,8 @@ hipError_t launch_decode(const Shape &s, const Rows &q, const Pages &pg, const i
     if (s.f16) decode_of<F16>(a, (uint32_t)blocks, stream);
     else decode_of<Bf16>(a, (uint32_t)blocks, stream);
     if (join) {
-        if (s.f16) k_attn_decode_join<F16><<<dim3((uint32_t)join), dim3(kJoinThreads), 0, stream>>>(a, weight_blocks);
-        else k_attn_decode_join<Bf16><<<dim3((uint32_t)join), dim3(kJoinThreads), 0, stream>>>(a, weight_blocks);
+        if (s.f16) k_attn_decode_join<F16><<<dim3((uint32_t)join), dim3(kJoinThreads), 0, stream>>>(a, weight_blocks, dims);
+        else k_attn_decode_join<Bf16><<<dim3((uint32_t)join), dim3(kJoinThreads), 0, stream>>>(a, weight_blocks, dims);
     }
     return hipGetLastError();
 }

@@ -6,6 +6,7 @@
 //             C: column l % 32, register i is row (i / 4) * 8 + (l / 32) * 4 + i % 4
 //   16x16x32  A: row l % 16, k = (l / 16) * 8 .. + 7     B: column l % 16, the same k
 //             C: column l % 16, register i is row (l / 16) * 4 + i
+//   16x16x16  A and B: k = (l / 16) * 4 .. + 3, C the same
 // The k of a product may be in any order as long as A and B agree on it: the kernels compute
 // scores transposed (keys as rows), so that the registers of a C tile, rounded to 2 bytes, are
 // the B fragment of the product with the values, whose A fragment takes its keys in that order.
@@ -28,6 +29,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 #define IBP_LDS(T) __attribute__((address_space(3))) T
@@ -46,6 +48,10 @@ struct Bf16 {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c,
                                                        0, 0, 0);
     }
+    static __device__ __forceinline__ f32x4 mfma16(u32x2 a, u32x2 b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, a), __builtin_bit_cast(s16x4, b), c, 0,
+                                                         0, 0);
+    }
     static __device__ __forceinline__ uint32_t pack(float x, float y) {   // round to nearest even
         const f32x2 v = {x, y};
         return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
@@ -62,6 +68,9 @@ struct F16 {
     static __device__ __forceinline__ f32x4 mfma16(Frag a, Frag b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0,
                                                       0, 0);
+    }
+    static __device__ __forceinline__ f32x4 mfma16(u32x2 a, u32x2 b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(f16x4, a), __builtin_bit_cast(f16x4, b), c, 0, 0, 0);
     }
     static __device__ __forceinline__ uint32_t pack(float x, float y) {
         const f32x2 v = {x, y};
