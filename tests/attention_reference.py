@@ -73,19 +73,21 @@ def evict(weights, positions, lens, next_positions, budget, recent):
     """Per (sequence, head): the slot whose content each of the first m slots has afterwards."""
     import math
     result = []
-    for b in range(weights.shape[0]):
+    weights, positions = weights.tolist(), positions.tolist()
+    for b in range(len(weights)):
         heads = []
-        for h in range(weights.shape[1]):
+        for h in range(len(weights[b])):
             n = lens[b]
             m = min(n, budget)
             rank = []
             for i in range(n):
-                w = weights[b, h, i].item()
-                guarded = positions[b, h, i].item() >= next_positions[b] - recent
-                rank.append((not guarded, NEG * -1 if math.isnan(w) else -w if not guarded else 0.0, i))
+                w = weights[b][h][i]
+                guarded = positions[b][h][i] >= next_positions[b] - recent
+                rank.append((not guarded, 0.0 if guarded else -NEG if math.isnan(w) else -w, i))
             kept = sorted(i for _, _, i in sorted(rank)[:m])
             source = list(range(m))
-            holes = [i for i in range(m) if i not in set(kept)]
+            stay = set(kept)
+            holes = [i for i in range(m) if i not in stay]
             for to, of in zip(holes, [i for i in kept if i >= m]):
                 source[to] = of
             heads.append(source)

@@ -255,6 +255,20 @@ def test_evict_sizes(ibp, kind, dim, page, n, budget):
     check_evict(c, weights, positions, [n], budget, budget // 4, got)
 
 
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("n,budget", [(4096, 4000), (4097, 7), (32768, 20000), (32769, 32700), (40000, 1)])
+def test_evict_long(ibp, n, budget, in_place):
+    """Lengths on both sides of what is held in registers, weights of few values beside many ties."""
+    c = Cache(BF16, 2, 8, [70, 3], 256, seed=1)      # (its rows are set below: two long heads are slow to draw one by one)
+    c.lens, c.per = [n, n - 1000], -(-n // 256)
+    c.k, c.v = (torch.randn(2 * c.per, 2, 256, 8, generator=torch.Generator().manual_seed(i)).to(BF16) for i in (1, 2))
+    c.table = torch.randperm(2 * c.per, generator=torch.Generator().manual_seed(3)).view(2, c.per).to(torch.int32)
+    weights, positions = arrays(c, seed=budget)
+    weights[0, 1] = (weights[0, 1] * 2).round()
+    got = run_evict(ibp, c, weights, positions, c.lens, budget, budget // 3, in_place)
+    check_evict(c, weights, positions, c.lens, budget, budget // 3, got, in_place)
+
+
 def test_evict_ties_and_special_weights(ibp):
     """Equal weights go by the lowest slot; NaN ranks as -inf, -0 as 0, infinities where they belong."""
     c = Cache(BF16, 3, 64, [300, 300], 16, seed=1)
