@@ -455,11 +455,16 @@ typedef struct {
  *   lse_i = ln sum_j exp(x_ij),   out_i = sum_j exp(x_ij - lse_i) v_j.
  * A row that sees no key, or only scores of -inf, gives zeros and an lse of -inf. What a row
  * does not see has no effect on it, infinities and NaN included. d_lse ([q_heads][q rows])
- * may be null. Rows of q outside all sequences leave out and d_lse as they are.
+ * may be null. Rows of q outside all sequences leave out and d_lse as they are. Few rows
+ * against many keys are split along the keys and joined; their parts are in the workspace
+ * (0 bytes for other sizes, and then it may be null).
  */
+ibp_status ibp_attn_prompt_workspace(uint32_t q_heads, uint32_t head_dim, uint64_t q_rows, uint64_t k_rows,
+                                     uint32_t n_seqs, uint64_t *bytes);
 ibp_status ibp_attn_prompt(const ibp_attn *a, const ibp_rows *q, const ibp_rows *k, const ibp_rows *v,
                            const int32_t *d_q_starts, const int32_t *d_k_starts, uint32_t n_seqs,
-                           const ibp_rows *out, float *d_lse, void *stream);
+                           const ibp_rows *out, float *d_lse, void *workspace, uint64_t workspace_bytes,
+                           void *stream);
 
 /*
  * ibp_attn_key_weights -- the attention weight that every key received:

@@ -93,7 +93,7 @@ _SIGS = {
     "ibp_cache_reset_stats": [_vp],
     "ibp_cache_destroy": [_vp],
 }
-_ATTENTION = ("ibp_attn_prompt", "ibp_attn_key_weights_workspace", "ibp_attn_key_weights", "ibp_attn_decode_workspace",
+_ATTENTION = ("ibp_attn_prompt_workspace", "ibp_attn_prompt", "ibp_attn_key_weights_workspace", "ibp_attn_key_weights", "ibp_attn_decode_workspace",
               "ibp_attn_decode", "ibp_kv_evict_workspace", "ibp_kv_evict")     # in attention.py, on torch tensors
 EXPORTS = sorted(list(_SIGS) + list(_ATTENTION) + ["ibp_last_error", "ibp_version"])
 

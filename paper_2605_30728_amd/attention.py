@@ -37,7 +37,8 @@ class ibp_pages(ctypes.Structure):
 _p = ctypes.POINTER
 _vp = ctypes.c_void_p
 SIGS = {
-    "ibp_attn_prompt": [_p(ibp_attn), _p(ibp_rows), _p(ibp_rows), _p(ibp_rows), _vp, _vp, _u32, _p(ibp_rows), _vp, _vp],
+    "ibp_attn_prompt_workspace": [_u32, _u32, _u64, _u64, _u32, _p(_u64)],
+    "ibp_attn_prompt": [_p(ibp_attn), _p(ibp_rows), _p(ibp_rows), _p(ibp_rows), _vp, _vp, _u32, _p(ibp_rows), _vp, _vp, _u64, _vp],
     "ibp_attn_key_weights_workspace": [_u32, _u32, _u64, _p(_u64)],
     "ibp_attn_key_weights": [_p(ibp_attn), _p(ibp_rows), _p(ibp_rows), _vp, _vp, _u32, _vp, _vp, _vp, _u64, _vp],
     "ibp_attn_decode_workspace": [_u32, _u32, _u32, _u32, _u32, ctypes.c_int, _p(_u64)],
@@ -130,7 +131,9 @@ def _starts(q_starts, k_starts, device):
 def _space(workspace, need, device):
     """Address and size of the workspace, and what keeps it alive during the call."""
     if workspace is None:
-        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=f"cuda:{device}")
+        if need == 0:
+            return None, 0, None
+        workspace = torch.empty(need, dtype=torch.uint8, device=f"cuda:{device}")
     else:
         _array(workspace, "workspace", torch.uint8, device)
     return workspace.data_ptr(), workspace.numel(), workspace
@@ -142,7 +145,13 @@ def _stream(stream, device):
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
-def ibp_attn_prompt(q, k, v, q_starts, k_starts, out, lse=None, causal=True, scale=None, stream=None):
+def ibp_attn_prompt_workspace(q_heads, head_dim, q_rows, k_rows, n_seqs):
+    out = _u64(0)
+    check(lib().ibp_attn_prompt_workspace(q_heads, head_dim, q_rows, k_rows, n_seqs, out), "ibp_attn_prompt_workspace")
+    return out.value
+
+
+def ibp_attn_prompt(q, k, v, q_starts, k_starts, out, lse=None, causal=True, scale=None, workspace=None, stream=None):
     """Attention of packed sequences: q [rows][q_heads][dim] against k, v [rows][kv_heads][dim] into
     out (like q) and lse (float32 [q_heads][q rows], or None); starts are int32 on the GPU."""
     device = _device(q, "q")
@@ -157,8 +166,10 @@ def ibp_attn_prompt(q, k, v, q_starts, k_starts, out, lse=None, causal=True, sca
     n = _starts(q_starts, k_starts, device)
     lse_at = None if lse is None else _array(lse, "lse", torch.float32, device, (heads, q.shape[0]))
     a = _attn(q, kv_heads, dim, scale, causal)
-    check(lib().ibp_attn_prompt(a, rq, rk, rv, q_starts.data_ptr(), k_starts.data_ptr(), n, ro, lse_at, _stream(stream, device)),
-          "ibp_attn_prompt")
+    need = ibp_attn_prompt_workspace(heads, dim, q.shape[0], k.shape[0], n) if workspace is None else 0
+    at, size, held = _space(workspace, need, device)
+    check(lib().ibp_attn_prompt(a, rq, rk, rv, q_starts.data_ptr(), k_starts.data_ptr(), n, ro, lse_at, at, size,
+                                _stream(stream, device)), "ibp_attn_prompt")
 
 
 def ibp_attn_key_weights_workspace(q_heads, kv_heads, k_rows):

@@ -34,7 +34,9 @@ struct Packed {
 };
 
 hipError_t launch_prompt(const Shape &a, const Rows &q, const Rows &k, const Rows &v, const Packed &p, const Rows &out,
-                         float *lse, hipStream_t stream);
+                         float *lse, uint8_t *workspace, hipStream_t stream);
+// (none where the tiles fill the chip by themselves)
+uint64_t prompt_workspace(uint32_t q_heads, uint32_t dim, uint64_t q_rows, uint64_t k_rows, uint32_t n_seqs);
 
 // partial: [q_heads][k_rows] floats (unused, may be null, where group == 1).
 hipError_t launch_key_weights(const Shape &a, const Rows &q, const Rows &k, const Packed &p, const float *lse,

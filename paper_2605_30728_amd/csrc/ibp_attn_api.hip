@@ -111,7 +111,7 @@ ibp_status check_paged(uint32_t n_seqs, uint32_t kv_heads, const int32_t *d_lens
 
 ibp_status prompt_impl(const ibp_attn *a, const ibp_rows *q, const ibp_rows *k, const ibp_rows *v,
                        const int32_t *d_q_starts, const int32_t *d_k_starts, uint32_t n_seqs, const ibp_rows *out,
-                       float *d_lse, void *stream) {
+                       float *d_lse, void *workspace, uint64_t workspace_bytes, void *stream) {
     attn::Shape s;
     attn::Rows rq, rk, rv, ro;
     attn::Packed p;
@@ -123,7 +123,9 @@ ibp_status prompt_impl(const ibp_attn *a, const ibp_rows *q, const ibp_rows *k, 
     if (v->rows != k->rows) return fail(IBP_EINVAL, "k and v must have the same rows");
     if (out->rows < q->rows) return fail(IBP_ENOMEM, "out has fewer rows than q");
     IBP_TRY(take_starts(d_q_starts, d_k_starts, n_seqs, q->rows, k->rows, p));
-    return launched(attn::launch_prompt(s, rq, rk, rv, p, ro, d_lse, static_cast<hipStream_t>(stream)));
+    IBP_TRY(take_workspace(workspace, workspace_bytes, attn::prompt_workspace(s.q_heads, s.dim, q->rows, k->rows, n_seqs)));
+    return launched(attn::launch_prompt(s, rq, rk, rv, p, ro, d_lse, static_cast<uint8_t *>(workspace),
+                                        static_cast<hipStream_t>(stream)));
 }
 
 ibp_status key_weights_impl(const ibp_attn *a, const ibp_rows *q, const ibp_rows *k, const int32_t *d_q_starts,
@@ -210,11 +212,23 @@ using namespace ibp;
 
 extern "C" {
 
+ibp_status ibp_attn_prompt_workspace(uint32_t q_heads, uint32_t head_dim, uint64_t q_rows, uint64_t k_rows, uint32_t n_seqs,
+                                     uint64_t *bytes) {
+    clear_error();
+    if (!bytes) return fail(IBP_EINVAL, "bytes is null");
+    if (q_heads == 0 || q_heads > 65536 || head_dim == 0 || head_dim % 8 || head_dim > 256 || q_rows > kMaxRows || k_rows > kMaxRows)
+        return fail(IBP_EINVAL, "bad sizes");
+    *bytes = attn::prompt_workspace(q_heads, head_dim, q_rows, k_rows, n_seqs);
+    return IBP_OK;
+}
+
 ibp_status ibp_attn_prompt(const ibp_attn *a, const ibp_rows *q, const ibp_rows *k, const ibp_rows *v,
                            const int32_t *d_q_starts, const int32_t *d_k_starts, uint32_t n_seqs, const ibp_rows *out,
-                           float *d_lse, void *stream) {
+                           float *d_lse, void *workspace, uint64_t workspace_bytes, void *stream) {
     clear_error();
-    return guarded([&] { return prompt_impl(a, q, k, v, d_q_starts, d_k_starts, n_seqs, out, d_lse, stream); });
+    return guarded([&] {
+        return prompt_impl(a, q, k, v, d_q_starts, d_k_starts, n_seqs, out, d_lse, workspace, workspace_bytes, stream);
+    });
 }
 
 ibp_status ibp_attn_key_weights_workspace(uint32_t q_heads, uint32_t kv_heads, uint64_t k_rows, uint64_t *bytes) {

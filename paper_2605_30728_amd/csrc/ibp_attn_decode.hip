@@ -44,12 +44,6 @@ __device__ __forceinline__ int slots_of(const DecodeArgs &a, uint32_t seq) {
     return min(max(a.lens[seq], 0), (int)a.max_len);
 }
 
-// What a part with this reference and sum counts for beside the common reference; below zero: it
-// saw no key at all (one that only saw NaN has a reference of -inf too, but a sum of NaN).
-__device__ __forceinline__ float part_of(float ref, float sum, float top, float c) {
-    return ref == -__builtin_inff() ? (sum == 0.f ? -1.f : 1.f) : exp2_fast((ref - top) * c);
-}
-
 template <class T, int DIM, bool FULL>
 __global__ __launch_bounds__(64 * kWaves, 2) void k_attn_decode(DecodeArgs a) {
     constexpr int kChunk = chunk_slots<DIM>(), KT = kChunk / 16;

@@ -7,6 +7,8 @@
 #include "ibp_attn.hpp"
 #include "ibp_attn_wave.hpp"
 
+#include <algorithm>
+
 namespace ibp {
 namespace attn {
 
@@ -19,7 +21,10 @@ struct PromptArgs {
     Packed p;
     float *lse;
     uint32_t q_heads, kv_heads, group, dim;
-    uint32_t tiles;              // blocks per head: at least the tiles of all sequences
+    uint32_t tiles;              // per head: at least the tiles of all sequences
+    uint32_t splits;             // blocks that share a tile's keys
+    f32x2 *stats;                // splits > 1: [split][q_heads][q rows] reference (in scores) and sum
+    float *partial;              //   [split][q_heads][q rows][dim]
     float scale, scale_log2;
     uint32_t causal;
 };
@@ -31,15 +36,21 @@ constexpr float kLazy = 8.f;     // how far (in powers of two) weights may excee
 template <int DIM>
 constexpr int key_tile() { return DIM <= 128 ? 64 : 32; }
 
+// What a block leaves of a row: the row's output and lse, or its part of them.
+__device__ __forceinline__ int64_t part_at(const PromptArgs &a, int split, int head, int row) {
+    return ((int64_t)split * a.q_heads + head) * a.p.q_rows + row;
+}
+
 // One row, key by key in 32 bits, by one wave: lanes are keys for the scores and columns for the
 // sum. Only for rows whose tiles hold infinities or NaN in places that the row does not see.
 template <class T, int DIM>
-__device__ void attend_row(const PromptArgs &a, int row, int head, const uint8_t *kp, const uint8_t *vp, int keys) {
+__device__ void attend_row(const PromptArgs &a, int row, int head, int split, const uint8_t *kp, const uint8_t *vp,
+                           int from, int keys) {
     const int lane = threadIdx.x & 63;
     const uint16_t *q = (const uint16_t *)a.q.data + (int64_t)row * a.q.row + (int64_t)head * a.q.head;
     const float inf = __builtin_inff();
     float m = -inf, l = 0.f, acc[(DIM + 63) / 64] = {};
-    for (int k0 = 0; k0 < keys; k0 += 64) {
+    for (int k0 = from; k0 < keys; k0 += 64) {
         float s = -inf;
         if (k0 + lane < keys) {
             const uint16_t *k = (const uint16_t *)kp + (int64_t)(k0 + lane) * a.k.row;
@@ -64,6 +75,14 @@ __device__ void attend_row(const PromptArgs &a, int row, int head, const uint8_t
                 if (lane + 64 * x < (int)a.dim) acc[x] = __builtin_fmaf(w, T::value(v[lane + 64 * x]), acc[x]);
         }
     }
+    if (a.splits > 1) {
+        const int64_t at = part_at(a, split, head, row);
+        if (lane == 0) a.stats[at] = f32x2{m, l};
+#pragma unroll
+        for (int x = 0; x < (DIM + 63) / 64; ++x)
+            if (lane + 64 * x < (int)a.dim) a.partial[at * a.dim + lane + 64 * x] = acc[x];
+        return;
+    }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     uint16_t *out = (uint16_t *)a.out.data + (int64_t)row * a.out.row + (int64_t)head * a.out.head;
 #pragma unroll
@@ -81,21 +100,23 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_prompt
 
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
 
-    // the head and tile of this block: the heads that share keys run on one XCD where they can
-    // be dealt out evenly, tiles with the most keys first
-    uint32_t head, t;
+    // the head, tile and split of this block: the heads that share keys run on one XCD where they
+    // can be dealt out evenly, tiles with the most keys first
+    uint32_t head, t, split;
     const uint32_t b = blockIdx.x;
     if (a.kv_heads % 8 == 0) {
-        const uint32_t i = b >> 3, per = a.group * a.tiles;
+        const uint32_t i = b >> 3, per = a.group * a.splits * a.tiles;
         head = ((b & 7) + 8 * (i / per)) * a.group + i % per % a.group;
-        t = i % per / a.group;
+        split = i % per / a.group % a.splits;
+        t = i % per / a.group / a.splits;
     } else {
         head = b % a.q_heads;
-        t = b / a.q_heads;
+        split = b / a.q_heads % a.splits;
+        t = b / a.q_heads / a.splits;
     }
     SeqTile st;
     if (!find_tile<false>(a.p.q_starts, a.p.k_starts, a.p.n_seqs, a.p.q_rows, a.p.k_rows, kBlockRows, t, st)) return;
-    const int tile = st.tiles - 1 - st.tile;
+    const int tile = st.rank;
     const int q_len = st.q_len, k_len = st.k_len;
     const int past = k_len - q_len;                            // causal: row i sees keys j <= i + past
     const int row = tile * kBlockRows + wave * 32 + col;
@@ -107,7 +128,8 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_prompt
     const int wave_any = a.causal ? min(max(wave_last + past + 1, 0), k_len) : k_len;    // keys that any of them sees
     const int block_last = min(tile * kBlockRows + kBlockRows - 1, q_len - 1);
     const int keys = a.causal ? min(max(block_last + past + 1, 0), k_len) : k_len;
-    const int n_tiles = (keys + N - 1) / N;
+    const int all_tiles = (keys + N - 1) / N, per_split = (all_tiles + a.splits - 1) / a.splits;
+    const int first_tile = min((int)split * per_split, all_tiles), n_tiles = min(first_tile + per_split, all_tiles);
 
     const uint32_t kv = head / a.group;
     const uint32_t k_stride = (uint32_t)a.k.row * 2, v_stride = (uint32_t)a.v.row * 2;
@@ -132,7 +154,7 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_prompt
         for (int i = 0; i < kLoads; ++i) load_to_lds(vr, at + kTileBytes + i * kWaves * 1024, v_off[i]);
     };
 
-    if (n_tiles > 0) load_tile(0, 0);
+    if (first_tile < n_tiles) load_tile(first_tile, first_tile & 1);
 
     Frag q[KS];
     {
@@ -149,7 +171,7 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_prompt
     for (int d = 0; d < DT; ++d) acc[d] = f32x16{};
 
     bool odd = false;
-    for (int n = 0; n < n_tiles; ++n) {
+    for (int n = first_tile; n < n_tiles; ++n) {
         tiles_loaded();
         if (n + 1 < n_tiles) load_tile(n + 1, (n + 1) & 1);
         const int key0 = n * N;
@@ -220,12 +242,27 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_prompt
     if (__any(odd)) {
         const int rows = min(q_len - (tile * kBlockRows + wave * 32), 32);
         for (int r = 0; r < rows; ++r)
-            attend_row<T, DIM>(a, st.q0 + row - col + r, head, kp, vp, uniform(__shfl(limit, r)));
+            attend_row<T, DIM>(a, st.q0 + row - col + r, head, split, kp, vp, first_tile * N,
+                               min(uniform(__shfl(limit, r)), n_tiles * N));
         return;
     }
 
     l = sum_halves(l);
     if (row >= q_len) return;
+    if (a.splits > 1) {
+        const int64_t at = part_at(a, split, head, st.q0 + row);
+        if (half == 0) a.stats[at] = f32x2{m, l};
+        float *pp = a.partial + at * a.dim;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int to = d * 32 + i * 8 + half * 4;
+                if (to < (int)a.dim)
+                    *reinterpret_cast<f32x4 *>(pp + to) = f32x4{acc[d][i * 4], acc[d][i * 4 + 1], acc[d][i * 4 + 2], acc[d][i * 4 + 3]};
+            }
+        return;
+    }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     uint8_t *op = (uint8_t *)a.out.data + ((int64_t)(st.q0 + row) * a.out.row + (int64_t)head * a.out.head) * 2;
 #pragma unroll
@@ -242,6 +279,49 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_prompt
         a.lse[(int64_t)head * a.p.q_rows + st.q0 + row] = l == 0.f ? -inf : m * a.scale + __logf(l);
 }
 
+// Joins the splits of 32 rows of a tile, four dims per thread:
+//   m = max_x m_x,  l = sum_x l_x 2^(m_x - m),  out = sum_x acc_x 2^(m_x - m) / l.
+constexpr int kMaxSplits = 8;
+
+template <class T>
+__global__ __launch_bounds__(256) void k_attn_prompt_join(PromptArgs a) {
+    const uint32_t b = blockIdx.x / (kBlockRows / 32), head = b % a.q_heads, t = b / a.q_heads;
+    SeqTile st;
+    if (!find_tile<false>(a.p.q_starts, a.p.k_starts, a.p.n_seqs, a.p.q_rows, a.p.k_rows, kBlockRows, t, st)) return;
+    const int row0 = st.rank * kBlockRows + blockIdx.x % (kBlockRows / 32) * 32, rows = min(st.q_len - row0, 32);
+    const int quads = a.dim / 4;
+    const float inf = __builtin_inff();
+    for (int i = threadIdx.x; i < rows * quads; i += 256) {
+        const int r = i / quads, d = (i - r * quads) * 4, row = st.q0 + row0 + r;
+        f32x2 s[kMaxSplits];
+        f32x4 x[kMaxSplits];
+        float top = -inf;
+#pragma unroll
+        for (int y = 0; y < kMaxSplits; ++y) {
+            const int64_t at = part_at(a, min(y, (int)a.splits - 1), head, row);
+            s[y] = a.stats[at];
+            x[y] = *reinterpret_cast<const f32x4 *>(a.partial + at * a.dim + d);
+            top = fmaxf(top, s[y][0]);
+        }
+        float sum = 0.f;
+        f32x4 o{};
+#pragma unroll
+        for (int y = 0; y < kMaxSplits; ++y) {
+            const float f = part_of(s[y][0], s[y][1], top, a.scale_log2);
+            if (y < (int)a.splits && !(f < 0.f)) {
+                sum += f * s[y][1];
+                o += f * x[y];
+            }
+        }
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        u32x2 w;
+        w[0] = T::pack(o[0] * inv, o[1] * inv);
+        w[1] = T::pack(o[2] * inv, o[3] * inv);
+        *reinterpret_cast<u32x2 *>((uint8_t *)a.out.data + ((int64_t)row * a.out.row + (int64_t)head * a.out.head + d) * 2) = w;
+        if (a.lse && d == 0) a.lse[(int64_t)head * a.p.q_rows + row] = sum == 0.f ? -inf : top * a.scale + __logf(sum);
+    }
+}
+
 template <class T>
 hipError_t prompt_of(const PromptArgs &a, uint32_t blocks, hipStream_t stream) {
     const dim3 grid(blocks), block(64 * kWaves);
@@ -249,19 +329,40 @@ hipError_t prompt_of(const PromptArgs &a, uint32_t blocks, hipStream_t stream) {
     else if (a.dim <= 96) k_attn_prompt<T, 96><<<grid, block, 0, stream>>>(a);
     else if (a.dim <= 128) k_attn_prompt<T, 128><<<grid, block, 0, stream>>>(a);
     else k_attn_prompt<T, 256><<<grid, block, 0, stream>>>(a);
+    if (a.splits > 1) k_attn_prompt_join<T><<<dim3(a.tiles * a.q_heads * (kBlockRows / 32)), dim3(256), 0, stream>>>(a);
     return hipGetLastError();
 }
 
+// What the tiles of all sequences come to at most.
+uint64_t tiles_of(uint64_t q_rows, uint64_t n_seqs) { return q_rows / kBlockRows + n_seqs; }
+
+// Blocks that share a tile's keys: as many as leave none of the 512 places of the chip empty, each
+// with at least 512 keys of a sequence of average length.
+uint32_t splits_of(uint32_t q_heads, uint64_t q_rows, uint64_t k_rows, uint64_t n_seqs) {
+    const uint64_t blocks = tiles_of(q_rows, n_seqs) * q_heads;
+    if (n_seqs == 0 || blocks == 0) return 1;
+    return (uint32_t)std::max<uint64_t>(std::min<uint64_t>({(uint64_t)kMaxSplits, 512 / blocks, k_rows / n_seqs / 512}), 1);
+}
+
+uint64_t up256(uint64_t x) { return (x + 255) / 256 * 256; }
+
 }  // namespace
 
+uint64_t prompt_workspace(uint32_t q_heads, uint32_t dim, uint64_t q_rows, uint64_t k_rows, uint32_t n_seqs) {
+    const uint64_t splits = splits_of(q_heads, q_rows, k_rows, n_seqs), parts = splits * q_heads * q_rows;
+    return splits > 1 ? up256(parts * 8) + up256(parts * dim * 4) : 0;
+}
+
 hipError_t launch_prompt(const Shape &s, const Rows &q, const Rows &k, const Rows &v, const Packed &p, const Rows &out,
-                         float *lse, hipStream_t stream) {
+                         float *lse, uint8_t *workspace, hipStream_t stream) {
     if (p.n_seqs == 0 || p.q_rows == 0) return hipSuccess;
-    const uint64_t tiles = p.q_rows / kBlockRows + (uint64_t)p.n_seqs;   // what all sequences need at most
-    const uint64_t blocks = tiles * s.q_heads;
+    const uint64_t tiles = tiles_of(p.q_rows, p.n_seqs);
+    const uint32_t splits = splits_of(s.q_heads, p.q_rows, p.k_rows, p.n_seqs);
+    const uint64_t blocks = tiles * s.q_heads * splits;
     if (blocks > kMaxGrid) return hipErrorInvalidConfiguration;
-    PromptArgs a{q, k, v, out, p, lse, s.q_heads, s.kv_heads, s.group, s.dim, (uint32_t)tiles, s.scale, s.scale_log2,
-                 s.causal ? 1u : 0u};
+    PromptArgs a{q, k, v, out, p, lse, s.q_heads, s.kv_heads, s.group, s.dim, (uint32_t)tiles, splits,
+                 (f32x2 *)workspace, (float *)(workspace + up256((uint64_t)splits * s.q_heads * p.q_rows * 8)), s.scale,
+                 s.scale_log2, s.causal ? 1u : 0u};
     return s.f16 ? prompt_of<F16>(a, (uint32_t)blocks, stream) : prompt_of<Bf16>(a, (uint32_t)blocks, stream);
 }
 

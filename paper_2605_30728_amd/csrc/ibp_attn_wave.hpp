@@ -16,6 +16,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include "ibp_wave.hpp"
+
 namespace ibp {
 namespace attn {
 namespace dev {
@@ -142,6 +144,12 @@ __device__ __forceinline__ u32x2 read_columns(const uint8_t *tile, int row, int 
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((IBP_LDS(s16x4) *)p));
 }
 
+// What a part with this reference and sum counts for beside the common reference; below zero: it
+// saw no key at all (one that only saw NaN has a reference of -inf too, but a sum of NaN).
+__device__ __forceinline__ float part_of(float ref, float sum, float top, float c) {
+    return ref == -__builtin_inff() ? (sum == 0.f ? -1.f : 1.f) : exp2_fast((ref - top) * c);
+}
+
 using Rsrc = __amdgpu_buffer_rsrc_t;
 
 // A descriptor of `bytes` bytes from p on: a load beyond them gives zeros.
@@ -185,10 +193,12 @@ __device__ __forceinline__ Frag load_head(const uint8_t *head, int d, int dim) {
     return Frag{in ? f[0] : 0, in ? f[1] : 0, in ? f[2] : 0, in ? f[3] : 0};
 }
 
-// The sequence and tile of block `t` where a packed sequence of n rows makes ceil(n / tile_rows)
-// tiles: every wave scans the starts, 64 sequences at a time. False: no such tile.
+// The sequence and tile of block `t`, where a packed sequence of n rows makes ceil(n / tile_rows)
+// tiles, `rank` the tile's number. Of up to 64 sequences the blocks come in falling order of rank
+// over all of them, so that where a tile's work grows with its rank the long ones are not left
+// for the end; of more, sequence by sequence. Every wave works this out by itself. False: no such tile.
 struct SeqTile {
-    int q0, q_len, k0, k_len, tile, tiles;
+    int q0, q_len, k0, k_len, rank, tiles;
 };
 __device__ __forceinline__ int clamp_row(int x, int rows) { return min(max(x, 0), rows); }
 
@@ -207,24 +217,44 @@ __device__ __forceinline__ bool find_tile(const int32_t *q_starts, const int32_t
         }
         const int n = max(BY_KEYS ? k1 - k0 : q1 - q0, 0);
         const int mine = (n + tile_rows - 1) / tile_rows;
-        int sum = mine;
+        const int sum = (int)::ibp::dev::wave_incl_scan((uint32_t)mine), all = __builtin_amdgcn_readlane(sum, 63);
+        if (t >= all) {
+            t -= all;
+            continue;
+        }
+        int at, rank;
+        if (n_seqs > 64) {
+            at = __builtin_ctzll(__ballot(sum > t));
+            rank = __builtin_amdgcn_readlane(mine, at) - 1 - (t - __builtin_amdgcn_readlane(sum - mine, at));
+        } else {
+            // lane i counts the sequences that have a tile of rank top - i, then 64 ranks further down
+            int top = mine;
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int y = __shfl_up(sum, d);
-            if (lane >= d) sum += y;
+            for (int d = 1; d < 64; d <<= 1) top = max(top, __shfl_xor(top, d));
+            int done = 0;
+            for (int first = uniform(top) - 1;; first -= 64) {
+                int have = 0;
+                for (int i = 0; i < n_seqs; ++i) have += __builtin_amdgcn_readlane(mine, i) > max(first - lane, -1) && first >= lane;
+                const int upto = done + (int)::ibp::dev::wave_incl_scan((uint32_t)have);
+                const uint64_t past = __ballot(upto > t);
+                if (past) {
+                    const int i = __builtin_ctzll(past);
+                    rank = first - i;
+                    const int nth = t - __builtin_amdgcn_readlane(upto - have, i);
+                    const uint64_t those = __ballot(mine > rank);
+                    at = __builtin_ctzll(__ballot(mine > rank && __popcll(those & ((1ull << lane) - 1)) == nth));
+                    break;
+                }
+                done = __builtin_amdgcn_readlane(upto, 63);
+            }
         }
-        const uint64_t past = __ballot(sum > t);
-        if (past) {
-            const int at = __builtin_ctzll(past);
-            out.tile = uniform(__shfl(t - (sum - mine), at));
-            out.tiles = uniform(__shfl(mine, at));
-            out.q0 = uniform(__shfl(q0, at));
-            out.q_len = uniform(__shfl(max(q1 - q0, 0), at));
-            out.k0 = uniform(__shfl(k0, at));
-            out.k_len = uniform(__shfl(max(k1 - k0, 0), at));
-            return true;
-        }
-        t -= uniform(__shfl(sum, 63));
+        out.rank = rank;
+        out.tiles = __builtin_amdgcn_readlane(mine, at);
+        out.q0 = __builtin_amdgcn_readlane(q0, at);
+        out.q_len = __builtin_amdgcn_readlane(max(q1 - q0, 0), at);
+        out.k0 = __builtin_amdgcn_readlane(k0, at);
+        out.k_len = __builtin_amdgcn_readlane(max(k1 - k0, 0), at);
+        return true;
     }
     return false;
 }

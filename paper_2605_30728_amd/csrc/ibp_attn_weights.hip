@@ -53,7 +53,7 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_key_we
     if (!find_tile<true>(a.p.q_starts, a.p.k_starts, a.p.n_seqs, a.p.q_rows, a.p.k_rows, kBlockKeys, t, st)) return;
     const int q_len = st.q_len, k_len = st.k_len, past = k_len - q_len;
     const uint32_t kv = head / a.group;
-    const int key0 = st.tile * kBlockKeys + wave * 64;
+    const int tile = st.tiles - 1 - st.rank, key0 = tile * kBlockKeys + wave * 64;   // (the first keys are seen by the most rows)
 
     Frag k[2][KS];
 #pragma unroll
@@ -85,7 +85,7 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_key_we
     };
 
     // the first row that sees a key of this block, and of this wave; the first that sees all of the wave's
-    const int first = a.causal ? max(st.tile * kBlockKeys - past, 0) : 0;
+    const int first = a.causal ? max(tile * kBlockKeys - past, 0) : 0;
     const int wave_any = a.causal ? max(key0 - past, 0) : 0;
     const int wave_all = a.causal ? max(min(key0 + 63, k_len - 1) - past, 0) : 0;
     const int n0 = first / N, n1 = (q_len + N - 1) / N;

@@ -10,7 +10,6 @@
 // new arrays; k_evict_move copies the K and V rows, or the first kernel does where they are few.
 #include "ibp_attn.hpp"
 #include "ibp_attn_wave.hpp"
-#include "ibp_wave.hpp"
 
 #include <algorithm>
 

@@ -33,7 +33,7 @@ def status(f, *args):
 
 
 def prompt(a=None, q=None, k=None, v=None, qs=A, ks=A, n=1, out=None):
-    return status("ibp_attn_prompt", a or attn(), q or rows(), k or rows(heads=2), v or rows(heads=2), qs, ks, n, out or rows(), A, None)
+    return status("ibp_attn_prompt", a or attn(), q or rows(), k or rows(heads=2), v or rows(heads=2), qs, ks, n, out or rows(), A, A, 1 << 30, None)
 
 
 BAD_ATTN = [dict(type=2), dict(q_heads=0), dict(kv_heads=0), dict(q_heads=5), dict(q_heads=65538), dict(head_dim=0), dict(head_dim=4),
@@ -73,8 +73,17 @@ def test_pages_are_checked(bad):
 
 def test_prompt_refuses():
     L = ibp.lib()
-    assert L.ibp_attn_prompt(None, rows(), rows(heads=2), rows(heads=2), A, A, 1, rows(), A, None) == ibp.IBP_EINVAL
-    assert L.ibp_attn_prompt(attn(), None, rows(heads=2), rows(heads=2), A, A, 1, rows(), A, None) == ibp.IBP_EINVAL
+    assert L.ibp_attn_prompt(None, rows(), rows(heads=2), rows(heads=2), A, A, 1, rows(), A, A, 0, None) == ibp.IBP_EINVAL
+    assert L.ibp_attn_prompt(attn(), None, rows(heads=2), rows(heads=2), A, A, 1, rows(), A, A, 0, None) == ibp.IBP_EINVAL
+    need = ctypes.c_uint64(0)
+    assert status("ibp_attn_prompt_workspace", 4, 64, 8, 4096, 1, need) == ibp.IBP_OK and need.value > 0
+    many = rows(4096, heads=2)
+    assert L.ibp_attn_prompt(attn(), rows(), many, many, A, A, 1, rows(), A, A, need.value - 1, None) == ibp.IBP_ENOMEM
+    assert L.ibp_attn_prompt(attn(), rows(), many, many, A, A, 1, rows(), A, None, 0, None) == ibp.IBP_EINVAL
+    assert status("ibp_attn_prompt_workspace", 4, 64, 4096, 4096, 100, need) == ibp.IBP_OK and need.value == 0
+    assert status("ibp_attn_prompt_workspace", 0, 64, 8, 8, 1, need) == ibp.IBP_EINVAL
+    assert status("ibp_attn_prompt_workspace", 4, 12, 8, 8, 1, need) == ibp.IBP_EINVAL
+    assert status("ibp_attn_prompt_workspace", 4, 64, 8, 8, 1, None) == ibp.IBP_EINVAL
     assert prompt(qs=None) == ibp.IBP_EINVAL and prompt(ks=None) == ibp.IBP_EINVAL and prompt(qs=A + 1) == ibp.IBP_EINVAL
     assert prompt(n=(1 << 24) + 1) == ibp.IBP_EINVAL
     assert prompt(v=rows(7, heads=2)) == ibp.IBP_EINVAL

@@ -93,6 +93,28 @@ def test_prompt_scales_and_moving_maximum(ibp, kind, scale):
     check_prompt(q, k, v, *lens, out, lse, scale=scale)
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("kind,heads,kv_heads,dim", [(BF16, 8, 8, 64), (F16, 2, 1, 80), (BF16, 3, 1, 128), (F16, 1, 1, 256)])
+def test_prompt_few_rows_many_keys(ibp, kind, heads, kv_heads, dim, causal):
+    """Split along the keys and joined; a sequence too short for its share of the splits beside a long one, and
+    a NaN and an infinity that the last rows see."""
+    lens = [40, 1, 130], [3100, 9, 2000]
+    assert ibp.ibp_attn_prompt_workspace(heads, dim, 171, 5109, 3) > 0
+    q, k, v = inputs(kind, heads, kv_heads, dim, *lens, seed=dim)
+    out, lse = run_prompt(ibp, q, k, v, *lens, causal=causal)
+    check_prompt(q, k, v, *lens, out, lse, causal=causal)
+    if causal:
+        clean = v.clone()
+        v[3099, 0, 1], v[5106, 0, 2] = float("inf"), float("nan")     # seen by row 39, and by rows 168 on
+        bad, bad_lse = run_prompt(ibp, q, k, v, *lens)
+        check_prompt(q, k, clean, *lens, out, bad_lse)                # (values have no part in an lse)
+        first = slice(0, heads // kv_heads)
+        assert (bad[39, first, 1].float() == float("inf")).all() and torch.isnan(bad[168:, first, 2]).all()
+        bad[39, first, 1], bad[168:, first, 2] = out[39, first, 1], out[168:, first, 2]
+        assert torch.isfinite(bad).all()
+        assert torch.allclose(bad.float(), out.float(), rtol=0.02, atol=0.02)
+
+
 @pytest.mark.parametrize("dim", [64, 128, 256])
 def test_prompt_many_sequences(ibp, dim):
     """More sequences than a wave has lanes, empty ones among them."""
