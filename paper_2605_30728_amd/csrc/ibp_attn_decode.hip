@@ -147,7 +147,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_attn_decode(DecodeArgs a) {
 #pragma unroll
         for (int i = 0; i < VL; ++i) {
             const int row = i * kRowsPer + lane / CH, ch = lane % CH;
-            *reinterpret_cast<Frag *>(vt + row * RB + ((ch ^ Tile<DIM>::columns(row)) << 4)) = vf[i];
+            *reinterpret_cast<Frag *>(vt + row * RB + ((ch ^ Tile<DIM>::template columns<16>(row)) << 4)) = vf[i];
         }
         if (chunk + kStep < to) load(chunk + kStep);
         if (a.scores && col < heads) {
@@ -184,11 +184,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_attn_decode(DecodeArgs a) {
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
             const int key = quarter * 4 + (col >> 2), at = d * 16 + (col & 3) * 4;
-            const u32x2 lo = read_columns<DIM>(vt, key, at);
+            const u32x2 lo = read_columns<DIM, 16>(vt, key, at);
             if constexpr (KT == 1) {
                 acc[d] = T::mfma16(lo, p[0], acc[d]);
             } else {
-                const u32x2 hi = read_columns<DIM>(vt, key + 16, at);
+                const u32x2 hi = read_columns<DIM, 16>(vt, key + 16, at);
                 acc[d] = T::mfma16(Frag{lo[0], lo[1], hi[0], hi[1]}, Frag{p[0][0], p[0][1], p[1][0], p[1][1]}, acc[d]);
             }
         }

@@ -8,6 +8,7 @@
 #include "ibp_attn_wave.hpp"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace ibp {
 namespace attn {
@@ -29,7 +30,7 @@ struct PromptArgs {
     uint32_t causal;
 };
 
-constexpr int kWaves = 4;
+constexpr int kWaves = 4;        // of a block, 32 rows each
 constexpr int kBlockRows = 32 * kWaves;
 constexpr float kLazy = 8.f;     // how far (in powers of two) weights may exceed 1
 
@@ -91,12 +92,116 @@ __device__ void attend_row(const PromptArgs &a, int row, int head, int split, co
     if (a.lse && lane == 0) a.lse[(int64_t)head * a.p.q_rows + row] = l == 0.f ? -inf : m * a.scale + __logf(l);
 }
 
+// A wave's share of a tile of K or V on its way into LDS.
+template <int LOADS>
+__device__ __forceinline__ void load_tile(uint8_t *__restrict to, Rsrc r, const uint32_t *off) {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) load_to_lds(r, to + i * kWaves * 1024, off[i]);
+}
+
+// A row's running state in its lanes (both halves of the wave agree on m).
+struct Running {
+    float m, l;                  // reference (a score) and sum of the weights relative to it
+    bool odd;                    // the row has to be done key by key
+};
+
+// The step of tile n for 32 rows of a wave: the weights p of its scores s, the products of the last tile's
+// weights `last` with its values (PV), and the next tile's scores `next` (S). The three do not depend on one
+// another, and the matrix unit only runs beside the vector unit where one wave's instructions
+// alternate: a matrix instruction that waits for its unit keeps the SIMD's other wave from issuing vector
+// instructions. So they are written down in turns, one matrix instruction, then its share of the
+// exponentials, and kept in that order. (Scores, softmax and values one after the other: TODO
+// us for 8,192 rows of 32 heads of 128; with the two waves of a SIMD in opposite phases: 538; in turns: TODO.)
+// kt, vt: the next tile's keys and the last one's values. On their way to k_to and v_to are the
+// keys after those and this tile's values. What is read and what is being loaded do not overlap (restrict
+// says so to the compiler, which else waits for the loads before it reads anything).
+template <class T, int DIM, int N, int LOADS, bool PV, bool S>
+__device__ __forceinline__ void step(const uint8_t *__restrict kt, const uint8_t *__restrict vt, uint8_t *__restrict k_to,
+                                     uint8_t *__restrict v_to, Rsrc kr, Rsrc vr, const uint32_t *k_off,
+                                     const uint32_t *v_off, const Frag *q, f32x16 *s, f32x16 *next, const Frag *last, Frag *p,
+                                     f32x16 *acc, Running &r, float c) {
+    constexpr int DT = DIM / 32, NT = N / 32, kPv = PV ? NT * 2 * DT : 0, kS = S ? NT * (DIM / 16) : 0;
+    constexpr int kAll = kPv + kS, kElems = S ? NT * 16 : 0;
+    const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+    const float inf = __builtin_inff();
+    if constexpr (S) {
+        load_tile<LOADS>(v_to, vr, v_off);
+        load_tile<LOADS>(k_to, kr, k_off);
+    }
+    auto fragment = [&](int f) {
+        if (f < kPv) {                   // 16 keys of 32 columns of the values, in the order of the weights' keys
+            const int x = f / DT, d = f % DT;
+            const int key = (x >> 1) * 32 + (x & 1) * 16 + half * 4 + ((lane & 15) >> 2);
+            const int at = d * 32 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+            const u32x2 lo = read_columns<DIM, 32>(vt, key, at), hi = read_columns<DIM, 32>(vt, key + 8, at);
+            return Frag{lo[0], lo[1], hi[0], hi[1]};
+        }
+        const int x = (f - kPv) / NT, j = (f - kPv) % NT;
+        return read_rows<DIM>(kt, j * 32 + col, x * 2 + half);
+    };
+    constexpr int kAhead = 4;            // fragments read ahead
+    Frag ahead[kAhead];
+#pragma unroll
+    for (int f = 0; f < kAhead && f < kAll; ++f) ahead[f] = fragment(f);
+
+    // the first four shares: the highest score; then the reference, which moves only where a score
+    // is far above it (any reference gives the same result); from then on the weights
+    constexpr int kTop = kAll >= 16 ? 4 : 1;
+    float top = -inf, to = r.m, mc = 0.f, sum = 0.f;
+#pragma unroll
+    for (int f = 0; f < kAll; ++f) {
+        __builtin_amdgcn_sched_barrier(0);
+        const Frag now = ahead[f % kAhead];
+        if (f + kAhead < kAll) ahead[f % kAhead] = fragment(f + kAhead);
+        if (f < kPv) {
+            acc[f % DT] = T::mfma32(now, last[f / DT], acc[f % DT]);
+        } else {
+            const int x = (f - kPv) / NT, j = (f - kPv) % NT;
+            next[j] = T::mfma32(now, q[x], x == 0 ? f32x16{} : next[j]);
+        }
+        if constexpr (S) {
+            if (f < kTop) {
+#pragma unroll
+                for (int e = f * kElems / kTop; e < (f + 1) * kElems / kTop; ++e) top = fmaxf(top, s[e / 16][e % 16]);
+            } else {
+                if (f == kTop) {
+                    top = max_halves(top);
+                    to = top > r.m + kLazy / c ? fmaxf(r.m, top) : r.m;
+                    mc = to == -inf ? 0.f : to * c;
+                }
+                constexpr int kShares = kAll - kTop;
+                const int e0 = (f - kTop) * (kElems / 2) / kShares * 2, e1 = (f - kTop + 1) * (kElems / 2) / kShares * 2;
+#pragma unroll
+                for (int e = e0; e < e1; e += 2) {
+                    const float a = exp2_fast(__builtin_fmaf(s[e / 16][e % 16], c, -mc));
+                    const float b = exp2_fast(__builtin_fmaf(s[e / 16][e % 16 + 1], c, -mc));
+                    sum += a + b;
+                    uint32_t w = T::pack(a, b);
+                    asm volatile("" : "+v"(w), "+v"(sum));       // (here, not where it is used)
+                    p[e / 8][e % 8 / 2] = w;
+                }
+            }
+        }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (S) {
+        if (__any(to != r.m)) {          // what there is so far is relative to the old reference
+            const float keep = r.m == -inf ? 0.f : exp2_fast((r.m - to) * c);
+            r.l *= keep;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) acc[d] *= keep;
+            r.m = to;
+        }
+        r.l += sum;
+    }
+}
+
 template <class T, int DIM>
 __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_prompt(PromptArgs a) {
     constexpr int N = key_tile<DIM>(), RB = Tile<DIM>::kRowBytes;
     constexpr int KS = DIM / 16, DT = DIM / 32, NT = N / 32;
     constexpr int kTileBytes = N * RB, kLoads = kTileBytes / 1024 / kWaves;
-    __shared__ __align__(128) uint8_t lds[4 * kTileBytes];    // K, V of two tiles
+    __shared__ __align__(128) uint8_t lds[4 * kTileBytes];    // K of two tiles, V of two tiles
 
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
 
@@ -123,9 +228,7 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_prompt
     const int seen_row = min(row, q_len - 1);
     const int limit = a.causal ? min(max(seen_row + past + 1, 0), k_len) : k_len;   // keys that this lane's row sees
     const int wave_first = min(tile * kBlockRows + wave * 32, q_len - 1);
-    const int wave_last = min(tile * kBlockRows + wave * 32 + 31, q_len - 1);
     const int wave_all = a.causal ? min(max(wave_first + past + 1, 0), k_len) : k_len;   // keys that all its rows see
-    const int wave_any = a.causal ? min(max(wave_last + past + 1, 0), k_len) : k_len;    // keys that any of them sees
     const int block_last = min(tile * kBlockRows + kBlockRows - 1, q_len - 1);
     const int keys = a.causal ? min(max(block_last + past + 1, 0), k_len) : k_len;
     const int all_tiles = (keys + N - 1) / N, per_split = (all_tiles + a.splits - 1) / a.splits;
@@ -143,18 +246,16 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_prompt
         k_off[i] = tile_source<DIM, true>(slot, k_stride, a.dim);
         v_off[i] = tile_source<DIM, false>(slot, v_stride, a.dim);
     }
-    auto load_tile = [&](int n, int buf) {
-        const int rows = min(k_len - n * N, N);
-        const Rsrc kr = descriptor(kp + (int64_t)n * N * k_stride, (rows - 1) * k_stride + a.dim * 2);
-        const Rsrc vr = descriptor(vp + (int64_t)n * N * v_stride, (rows - 1) * v_stride + a.dim * 2);
-        uint8_t *at = lds + buf * 2 * kTileBytes + wave * 1024;
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) load_to_lds(kr, at + i * kWaves * 1024, k_off[i]);
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) load_to_lds(vr, at + kTileBytes + i * kWaves * 1024, v_off[i]);
+    uint8_t *const lk = lds + wave * 1024, *const lv = lk + 2 * kTileBytes;
+    auto tile_of = [&](const uint8_t *p, uint32_t stride, int n) {       // (empty past the last tile: zeros)
+        const int rows = n < n_tiles ? min(k_len - n * N, N) : 0;
+        return descriptor(rows ? p + (int64_t)n * N * stride : p, rows ? (rows - 1) * stride + a.dim * 2 : 0);
     };
-
-    if (first_tile < n_tiles) load_tile(first_tile, first_tile & 1);
+    const bool some = first_tile < n_tiles;
+    if (some) {
+        load_tile<kLoads>(lk + (first_tile & 1) * kTileBytes, tile_of(kp, k_stride, first_tile), k_off);
+        load_tile<kLoads>(lk + (~first_tile & 1) * kTileBytes, tile_of(kp, k_stride, first_tile + 1), k_off);
+    }
 
     Frag q[KS];
     {
@@ -164,81 +265,65 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_prompt
     }
 
     const float inf = __builtin_inff();
-    const float c = a.scale_log2, lazy = kLazy / c;
-    float m = -inf, l = 0.f;
-    f32x16 acc[DT];
+    const float c = a.scale_log2;
+    Running r{-inf, 0.f, false};
+    f32x16 acc[DT], s0[NT], s1[NT];
+    Frag p0[NT * 2], p1[NT * 2];
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = f32x16{};
 
-    bool odd = false;
-    for (int n = first_tile; n < n_tiles; ++n) {
-        tiles_loaded();
-        if (n + 1 < n_tiles) load_tile(n + 1, (n + 1) & 1);
-        const int key0 = n * N;
-        if (key0 >= wave_any) continue;
-        const uint8_t *kt = lds + (n & 1) * 2 * kTileBytes, *vt = kt + kTileBytes;
-
-        f32x16 s[NT];
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            s[j] = f32x16{};
-#pragma unroll
-            for (int x = 0; x < KS; ++x)
-                s[j] = T::mfma32(read_rows<DIM>(kt, j * 32 + col, x * 2 + half), q[x], s[j]);
-        }
-        const bool masked = key0 + N > wave_all;
-        if (masked) {
-#pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (key0 + j * 32 + (i >> 2) * 8 + half * 4 + (i & 3) >= limit) s[j][i] = -inf;
-        }
-        float top = s[0][0];
+    // keys from a row's limit on have no score; `at` is tile n's first key
+    auto hide = [&](f32x16 *s, int at) {
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[j][i]);
-        top = max_halves(top);
-        if (__any(top > m + lazy)) {
-            const float next = fmaxf(m, top);
-            const float keep = m == -inf ? 0.f : exp2_fast((m - next) * c);
-            l *= keep;
-#pragma unroll
-            for (int d = 0; d < DT; ++d) acc[d] *= keep;
-            m = next;
-        }
-        const float mc = m == -inf ? 0.f : m * c;
-        Frag p[NT * 2];
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                s[j][i] = exp2_fast(__builtin_fmaf(s[j][i], c, -mc));
-                l += s[j][i];
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) p[j * 2 + i / 4][i % 4] = T::pack(s[j][i * 2], s[j][i * 2 + 1]);
-        }
-
-        if (masked) {
-            // a weight of zero must not meet an infinity or NaN: rows that do not see all of such
-            // a tile are done again, key by key
+            for (int i = 0; i < 16; ++i)
+                if (at + j * 32 + (i >> 2) * 8 + half * 4 + (i & 3) >= limit) s[j][i] = -inf;
+    };
+    // a weight of zero must not meet an infinity or NaN: rows that do not see all of such a tile are
+    // done again, key by key
+    auto look = [&](const uint8_t *vt) {
 #pragma unroll 4
-            for (int x = lane * 16; x < kTileBytes; x += 1024)
-                odd |= has_nonfinite<T>(*reinterpret_cast<const Frag *>(vt + x));
+        for (int x = lane * 16; x < kTileBytes; x += 1024)
+            r.odd |= has_nonfinite<T>(*reinterpret_cast<const Frag *>(vt + x));
+    };
+    auto tile_n = [&](auto pv, int n, f32x16 *s, f32x16 *next, const Frag *last, Frag *p) {
+        tiles_loaded();
+        const uint8_t *kt = lds + (~n & 1) * kTileBytes, *vt = lds + (2 + (~n & 1)) * kTileBytes;
+        if (n * N + N > wave_all) hide(s, n * N);
+        if (pv.value && n * N > wave_all) look(vt);
+        step<T, DIM, N, kLoads, pv.value, true>(kt, vt, lk + (n & 1) * kTileBytes, lv + (n & 1) * kTileBytes,
+                                                tile_of(kp, k_stride, n + 2), tile_of(vp, v_stride, n), k_off, v_off, q, s, next,
+                                                last, p, acc, r, c);
+    };
+    if (some) {
+        tiles_loaded();
+#pragma unroll
+        for (int j = 0; j < NT; ++j) s0[j] = f32x16{};
+#pragma unroll
+        for (int x = 0; x < KS; ++x)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+                s0[j] = T::mfma32(read_rows<DIM>(lds + (first_tile & 1) * kTileBytes, j * 32 + col, x * 2 + half), q[x], s0[j]);
+        tile_n(std::false_type{}, first_tile, s0, s1, p1, p0);
+        for (int n = first_tile + 1; n < n_tiles; n += 2) {
+            tile_n(std::true_type{}, n, s1, s0, p0, p1);
+            if (n + 1 < n_tiles) tile_n(std::true_type{}, n + 1, s0, s1, p1, p0);
         }
+        tiles_loaded();                  // the last tile's values
+        const uint8_t *vt = lds + (2 + (~n_tiles & 1)) * kTileBytes;
+        if (n_tiles * N > wave_all) look(vt);
+        const bool even = (n_tiles - first_tile) & 1;        // whose weights the last tile left
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
+        for (int x = 0; x < NT * 2; ++x)
 #pragma unroll
-            for (int x = 0; x < NT * 2; ++x) {
-                // 16 keys of 32 columns, in the order of p's keys
-                const int key = (x >> 1) * 32 + (x & 1) * 16 + half * 4 + ((lane & 15) >> 2);
-                const int at = d * 32 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
-                const u32x2 lo = read_columns<DIM>(vt, key, at), hi = read_columns<DIM>(vt, key + 8, at);
-                acc[d] = T::mfma32(Frag{lo[0], lo[1], hi[0], hi[1]}, p[x], acc[d]);
-            }
+            for (int i = 0; i < 4; ++i) p0[x][i] = even ? p0[x][i] : p1[x][i];
+        step<T, DIM, N, kLoads, true, false>(nullptr, vt, nullptr, nullptr, tile_of(kp, 0, n_tiles), tile_of(vp, 0, n_tiles), k_off,
+                                             v_off, q, s0, s1, p0, p1, acc, r, c);
     }
+    const float m = r.m;
+    float l = r.l;
+    const bool odd = r.odd;
     if (__any(odd)) {
         const int rows = min(q_len - (tile * kBlockRows + wave * 32), 32);
         for (int r = 0; r < rows; ++r)
@@ -285,10 +370,11 @@ constexpr int kMaxSplits = 8;
 
 template <class T>
 __global__ __launch_bounds__(256) void k_attn_prompt_join(PromptArgs a) {
-    const uint32_t b = blockIdx.x / (kBlockRows / 32), head = b % a.q_heads, t = b / a.q_heads;
+    constexpr int block_rows = kBlockRows, parts = block_rows / 32;
+    const uint32_t b = blockIdx.x / parts, head = b % a.q_heads, t = b / a.q_heads;
     SeqTile st;
-    if (!find_tile<false>(a.p.q_starts, a.p.k_starts, a.p.n_seqs, a.p.q_rows, a.p.k_rows, kBlockRows, t, st)) return;
-    const int row0 = st.rank * kBlockRows + blockIdx.x % (kBlockRows / 32) * 32, rows = min(st.q_len - row0, 32);
+    if (!find_tile<false>(a.p.q_starts, a.p.k_starts, a.p.n_seqs, a.p.q_rows, a.p.k_rows, block_rows, t, st)) return;
+    const int row0 = st.rank * block_rows + blockIdx.x % parts * 32, rows = min(st.q_len - row0, 32);
     const int quads = a.dim / 4;
     const float inf = __builtin_inff();
     for (int i = threadIdx.x; i < rows * quads; i += 256) {
@@ -329,15 +415,15 @@ hipError_t prompt_of(const PromptArgs &a, uint32_t blocks, hipStream_t stream) {
     else if (a.dim <= 96) k_attn_prompt<T, 96><<<grid, block, 0, stream>>>(a);
     else if (a.dim <= 128) k_attn_prompt<T, 128><<<grid, block, 0, stream>>>(a);
     else k_attn_prompt<T, 256><<<grid, block, 0, stream>>>(a);
-    if (a.splits > 1) k_attn_prompt_join<T><<<dim3(a.tiles * a.q_heads * (kBlockRows / 32)), dim3(256), 0, stream>>>(a);
+    if (a.splits > 1) k_attn_prompt_join<T><<<dim3(a.tiles * a.q_heads * kWaves), dim3(256), 0, stream>>>(a);
     return hipGetLastError();
 }
 
 // What the tiles of all sequences come to at most.
 uint64_t tiles_of(uint64_t q_rows, uint64_t n_seqs) { return q_rows / kBlockRows + n_seqs; }
 
-// Blocks that share a tile's keys: as many as leave none of the 512 places of the chip empty, each
-// with at least 512 keys of a sequence of average length.
+// Blocks that share a tile's keys: as many as leave none of the chip's 512 places empty, each with at least 512 keys of a
+// sequence of average length.
 uint32_t splits_of(uint32_t q_heads, uint64_t q_rows, uint64_t k_rows, uint64_t n_seqs) {
     const uint64_t blocks = tiles_of(q_rows, n_seqs) * q_heads;
     if (n_seqs == 0 || blocks == 0) return 1;

@@ -110,23 +110,29 @@ __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirs
 
 // Rows of a head of DIM values in LDS, as 16-byte chunks whose places are permuted within the
 // row so that the lanes of one read spread over all banks: `rows` for reads of one chunk of many
-// consecutive rows (a fragment's own rows), `columns` for transposing reads (64 bytes of eight
-// consecutive rows). Rows are 128, 256 or 512 bytes wide (96 values are padded to 256 bytes).
+// consecutive rows (a fragment's own rows), `columns` for transposing reads (half a wave at a time
+// 32 or 64 bytes of consecutive rows: WIDE 16 or 32 columns of eight or four of them). Rows are 128, 256
+// or 512 bytes wide (96 values are padded to 256 bytes).
 template <int DIM>
 struct Tile {
     static constexpr int kRowBytes = DIM <= 64 ? 128 : DIM <= 128 ? 256 : 512;
     static constexpr int kChunks = kRowBytes / 16;
     static __device__ __forceinline__ int rows(int row) { return DIM <= 64 ? (row >> 1) & 7 : row & 15; }
-    static __device__ __forceinline__ int columns(int row) { return DIM <= 64 ? ((row >> 1) & 1) << 2 : (row & 7) << 1; }
+    template <int WIDE>
+    static __device__ __forceinline__ int columns(int row) {
+        if (WIDE == 32) return DIM <= 64 ? ((row >> 1) & 1) << 2 : (row & 3) << 2;
+        return DIM <= 64 ? ((row >> 1) & 3) << 1 : (row & 7) << 1;
+    }
 };
 
 // Byte offset, in a tensor of `stride` bytes per row, that a lane loads for 16-byte chunk
 // `slot` of a tile; out of every tile's range where the chunk holds no values of the head.
 constexpr uint32_t kNowhere = 0x80000000u;
+// ROWS: laid out as `rows`, else as 32 wide `columns`.
 template <int DIM, bool ROWS>
 __device__ __forceinline__ uint32_t tile_source(int slot, uint32_t stride, int dim) {
     const int row = slot / Tile<DIM>::kChunks;
-    const int c = (slot % Tile<DIM>::kChunks) ^ (ROWS ? Tile<DIM>::rows(row) : Tile<DIM>::columns(row));
+    const int c = (slot % Tile<DIM>::kChunks) ^ (ROWS ? Tile<DIM>::rows(row) : Tile<DIM>::template columns<32>(row));
     return c * 8 < dim ? row * stride + c * 16 : kNowhere;
 }
 
@@ -138,9 +144,9 @@ __device__ __forceinline__ Frag read_rows(const uint8_t *tile, int row, int c) {
 
 // Four rows of 16 values, transposed over 16 lanes: lane i of the 16 gets value i of the rows
 // r0 .. r0 + 3, when it passes row r0 + i / 4 and column c0 + (i % 4) * 4 here.
-template <int DIM>
+template <int DIM, int WIDE>
 __device__ __forceinline__ u32x2 read_columns(const uint8_t *tile, int row, int col) {
-    const uint8_t *p = tile + row * Tile<DIM>::kRowBytes + (((col >> 3) ^ Tile<DIM>::columns(row)) << 4) + (col & 7) * 2;
+    const uint8_t *p = tile + row * Tile<DIM>::kRowBytes + (((col >> 3) ^ Tile<DIM>::template columns<WIDE>(row)) << 4) + (col & 7) * 2;
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((IBP_LDS(s16x4) *)p));
 }
 
