@@ -472,10 +472,11 @@ ibp_status ibp_attn_prompt(const ibp_attn *a, const ibp_rows *q, const ibp_rows 
  *                     of exp(x_ij - d_lse[h][i]),
  * with d_lse as ibp_attn_prompt left it for the same q, k, starts and parameters (a row of
  * lse -inf gives nothing). d_weights is [kv_heads][k rows]; rows of k outside all sequences
- * leave theirs as they are. The workspace holds the query heads' own sums (none for
- * q_heads == kv_heads).
+ * leave theirs as they are. The workspace holds the sums of blocks and query heads before
+ * they are added up; what n_seqs = 1 needs is enough for any number of sequences.
  */
-ibp_status ibp_attn_key_weights_workspace(uint32_t q_heads, uint32_t kv_heads, uint64_t k_rows, uint64_t *bytes);
+ibp_status ibp_attn_key_weights_workspace(uint32_t q_heads, uint32_t kv_heads, uint64_t k_rows, uint32_t n_seqs,
+                                          uint64_t *bytes);
 ibp_status ibp_attn_key_weights(const ibp_attn *a, const ibp_rows *q, const ibp_rows *k, const int32_t *d_q_starts,
                                 const int32_t *d_k_starts, uint32_t n_seqs, const float *d_lse, float *d_weights,
                                 void *workspace, uint64_t workspace_bytes, void *stream);

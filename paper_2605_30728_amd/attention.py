@@ -39,7 +39,7 @@ _vp = ctypes.c_void_p
 SIGS = {
     "ibp_attn_prompt_workspace": [_u32, _u32, _u64, _u64, _u32, _p(_u64)],
     "ibp_attn_prompt": [_p(ibp_attn), _p(ibp_rows), _p(ibp_rows), _p(ibp_rows), _vp, _vp, _u32, _p(ibp_rows), _vp, _vp, _u64, _vp],
-    "ibp_attn_key_weights_workspace": [_u32, _u32, _u64, _p(_u64)],
+    "ibp_attn_key_weights_workspace": [_u32, _u32, _u64, _u32, _p(_u64)],
     "ibp_attn_key_weights": [_p(ibp_attn), _p(ibp_rows), _p(ibp_rows), _vp, _vp, _u32, _vp, _vp, _vp, _u64, _vp],
     "ibp_attn_decode_workspace": [_u32, _u32, _u32, _u32, _u32, ctypes.c_int, _p(_u64)],
     "ibp_attn_decode": [_p(ibp_attn), _p(ibp_rows), _p(ibp_pages), _vp, _u32, _p(ibp_rows), _vp, _vp, _u64, _vp, _u64, _vp],
@@ -172,9 +172,9 @@ def ibp_attn_prompt(q, k, v, q_starts, k_starts, out, lse=None, causal=True, sca
                                 _stream(stream, device)), "ibp_attn_prompt")
 
 
-def ibp_attn_key_weights_workspace(q_heads, kv_heads, k_rows):
+def ibp_attn_key_weights_workspace(q_heads, kv_heads, k_rows, n_seqs=1):
     out = _u64(0)
-    check(lib().ibp_attn_key_weights_workspace(q_heads, kv_heads, k_rows, out), "ibp_attn_key_weights_workspace")
+    check(lib().ibp_attn_key_weights_workspace(q_heads, kv_heads, k_rows, n_seqs, out), "ibp_attn_key_weights_workspace")
     return out.value
 
 
@@ -192,7 +192,7 @@ def ibp_attn_key_weights(q, k, q_starts, k_starts, lse, weights, causal=True, sc
     lse_at = _array(lse, "lse", torch.float32, device, (heads, q.shape[0]))
     weights_at = _array(weights, "weights", torch.float32, device, (kv_heads, k.shape[0]))
     a = _attn(q, kv_heads, dim, scale, causal)
-    need = ibp_attn_key_weights_workspace(heads, kv_heads, k.shape[0]) if workspace is None else 0
+    need = ibp_attn_key_weights_workspace(heads, kv_heads, k.shape[0], n) if workspace is None else 0
     at, size, held = _space(workspace, need, device)
     check(lib().ibp_attn_key_weights(a, rq, rk, q_starts.data_ptr(), k_starts.data_ptr(), n, lse_at, weights_at, at, size,
                                      _stream(stream, device)), "ibp_attn_key_weights")

@@ -38,7 +38,8 @@ hipError_t launch_prompt(const Shape &a, const Rows &q, const Rows &k, const Row
 // (none where the tiles fill the chip by themselves)
 uint64_t prompt_workspace(uint32_t q_heads, uint32_t dim, uint64_t q_rows, uint64_t k_rows, uint32_t n_seqs);
 
-// partial: [q_heads][k_rows] floats (unused, may be null, where group == 1).
+// partial: the workspace (unused, may be null, where it has 0 bytes).
+uint64_t key_weights_workspace(uint32_t q_heads, uint32_t kv_heads, uint64_t k_rows, uint32_t n_seqs);
 hipError_t launch_key_weights(const Shape &a, const Rows &q, const Rows &k, const Packed &p, const float *lse,
                               float *weights, float *partial, hipStream_t stream);
 

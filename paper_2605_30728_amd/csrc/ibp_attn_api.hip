@@ -93,10 +93,6 @@ ibp_status launched(hipError_t e) {
     return fail(IBP_EHIP, std::string("attention kernel: ") + hipGetErrorString(e));
 }
 
-uint64_t weights_workspace(uint32_t q_heads, uint32_t kv_heads, uint64_t k_rows) {
-    return q_heads == kv_heads ? 0 : (uint64_t)q_heads * k_rows * sizeof(float);
-}
-
 ibp_status check_paged(uint32_t n_seqs, uint32_t kv_heads, const int32_t *d_lens) {
     if ((uint64_t)n_seqs * kv_heads > attn::kMaxGrid) return fail(IBP_EINVAL, "too many sequences for one call");
     if (n_seqs && !d_lens) return fail(IBP_EINVAL, "sequence lengths are null");
@@ -140,7 +136,7 @@ ibp_status key_weights_impl(const ibp_attn *a, const ibp_rows *q, const ibp_rows
     IBP_TRY(take_starts(d_q_starts, d_k_starts, n_seqs, q->rows, k->rows, p));
     if (q->rows && !d_lse) return fail(IBP_EINVAL, "lse is null");
     if (k->rows && !d_weights) return fail(IBP_EINVAL, "weights are null");
-    IBP_TRY(take_workspace(workspace, workspace_bytes, weights_workspace(s.q_heads, s.kv_heads, k->rows)));
+    IBP_TRY(take_workspace(workspace, workspace_bytes, attn::key_weights_workspace(s.q_heads, s.kv_heads, k->rows, n_seqs)));
     return launched(attn::launch_key_weights(s, rq, rk, p, d_lse, d_weights, static_cast<float *>(workspace),
                                              static_cast<hipStream_t>(stream)));
 }
@@ -231,12 +227,13 @@ ibp_status ibp_attn_prompt(const ibp_attn *a, const ibp_rows *q, const ibp_rows 
     });
 }
 
-ibp_status ibp_attn_key_weights_workspace(uint32_t q_heads, uint32_t kv_heads, uint64_t k_rows, uint64_t *bytes) {
+ibp_status ibp_attn_key_weights_workspace(uint32_t q_heads, uint32_t kv_heads, uint64_t k_rows, uint32_t n_seqs,
+                                          uint64_t *bytes) {
     clear_error();
     if (!bytes) return fail(IBP_EINVAL, "bytes is null");
     if (kv_heads == 0 || q_heads == 0 || q_heads % kv_heads || q_heads > 65536 || k_rows > kMaxRows)
         return fail(IBP_EINVAL, "bad sizes");
-    *bytes = weights_workspace(q_heads, kv_heads, k_rows);
+    *bytes = attn::key_weights_workspace(q_heads, kv_heads, k_rows, n_seqs);
     return IBP_OK;
 }
 

@@ -110,8 +110,8 @@ struct Running {
 // another, and the matrix unit only runs beside the vector unit where one wave's instructions
 // alternate: a matrix instruction that waits for its unit keeps the SIMD's other wave from issuing vector
 // instructions. So they are written down in turns, one matrix instruction, then its share of the
-// exponentials, and kept in that order. (Scores, softmax and values one after the other: TODO
-// us for 8,192 rows of 32 heads of 128; with the two waves of a SIMD in opposite phases: 538; in turns: TODO.)
+// exponentials, and kept in that order. (Scores, softmax and values one after the other: 538
+// us for 8,192 rows of 32 heads of 128; with the two waves of a SIMD in opposite phases: 538; in turns: 508.)
 // kt, vt: the next tile's keys and the last one's values. On their way to k_to and v_to are the
 // keys after those and this tile's values. What is read and what is being loaded do not overlap (restrict
 // says so to the compiler, which else waits for the loads before it reads anything).
@@ -274,11 +274,12 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_prompt
 
     // keys from a row's limit on have no score; `at` is tile n's first key
     auto hide = [&](f32x16 *s, int at) {
+        const int end = limit - at - half * 4;
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                if (at + j * 32 + (i >> 2) * 8 + half * 4 + (i & 3) >= limit) s[j][i] = -inf;
+                if (j * 32 + (i >> 2) * 8 + (i & 3) >= end) s[j][i] = -inf;
     };
     // a weight of zero must not meet an infinity or NaN: rows that do not see all of such a tile are
     // done again, key by key

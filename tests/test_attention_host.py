@@ -98,11 +98,14 @@ def test_key_weights_refuse():
     assert call(lse=None) == ibp.IBP_EINVAL and call(w=None) == ibp.IBP_EINVAL and call(s=None) == ibp.IBP_EINVAL
     assert call(s=A + 4) == ibp.IBP_EINVAL
     need = ctypes.c_uint64(0)
-    assert status("ibp_attn_key_weights_workspace", 4, 2, 8, need) == ibp.IBP_OK and need.value > 0
+    assert status("ibp_attn_key_weights_workspace", 4, 2, 8, 1, need) == ibp.IBP_OK and need.value > 0
     assert call(sb=need.value - 1) == ibp.IBP_ENOMEM
-    assert status("ibp_attn_key_weights_workspace", 4, 4, 8, need) == ibp.IBP_OK and need.value == 0
-    assert status("ibp_attn_key_weights_workspace", 4, 3, 8, need) == ibp.IBP_EINVAL
-    assert status("ibp_attn_key_weights_workspace", 4, 2, 8, None) == ibp.IBP_EINVAL
+    most = need.value
+    for n in (2, 7, 31, 32, 1000):
+        assert status("ibp_attn_key_weights_workspace", 4, 2, 8, n, need) == ibp.IBP_OK and need.value <= most
+    assert status("ibp_attn_key_weights_workspace", 4, 4, 8, 32, need) == ibp.IBP_OK and need.value == 0
+    assert status("ibp_attn_key_weights_workspace", 4, 3, 8, 1, need) == ibp.IBP_EINVAL
+    assert status("ibp_attn_key_weights_workspace", 4, 2, 8, 1, None) == ibp.IBP_EINVAL
 
 
 def test_decode_refuses():
