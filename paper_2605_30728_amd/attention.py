@@ -128,12 +128,17 @@ def _starts(q_starts, k_starts, device):
     return q_starts.numel() - 1
 
 
-def _space(workspace, need, device):
-    """Address and size of the workspace, and what keeps it alive during the call."""
+def _space(workspace, need, device, stream):
+    """Address and size of the workspace, and what keeps it alive during the call. Memory that is taken here
+    belongs to the call's stream: what is given back is reused only behind the call's kernels."""
     if workspace is None:
         if need == 0:
             return None, 0, None
-        workspace = torch.empty(need, dtype=torch.uint8, device=f"cuda:{device}")
+        if stream is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=f"cuda:{device}")
+        else:
+            with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
+                workspace = torch.empty(need, dtype=torch.uint8, device=f"cuda:{device}")
     else:
         _array(workspace, "workspace", torch.uint8, device)
     return workspace.data_ptr(), workspace.numel(), workspace
@@ -167,7 +172,7 @@ def ibp_attn_prompt(q, k, v, q_starts, k_starts, out, lse=None, causal=True, sca
     lse_at = None if lse is None else _array(lse, "lse", torch.float32, device, (heads, q.shape[0]))
     a = _attn(q, kv_heads, dim, scale, causal)
     need = ibp_attn_prompt_workspace(heads, dim, q.shape[0], k.shape[0], n) if workspace is None else 0
-    at, size, held = _space(workspace, need, device)
+    at, size, held = _space(workspace, need, device, stream)
     check(lib().ibp_attn_prompt(a, rq, rk, rv, q_starts.data_ptr(), k_starts.data_ptr(), n, ro, lse_at, at, size,
                                 _stream(stream, device)), "ibp_attn_prompt")
 
@@ -193,7 +198,7 @@ def ibp_attn_key_weights(q, k, q_starts, k_starts, lse, weights, causal=True, sc
     weights_at = _array(weights, "weights", torch.float32, device, (kv_heads, k.shape[0]))
     a = _attn(q, kv_heads, dim, scale, causal)
     need = ibp_attn_key_weights_workspace(heads, kv_heads, k.shape[0], n) if workspace is None else 0
-    at, size, held = _space(workspace, need, device)
+    at, size, held = _space(workspace, need, device, stream)
     check(lib().ibp_attn_key_weights(a, rq, rk, q_starts.data_ptr(), k_starts.data_ptr(), n, lse_at, weights_at, at, size,
                                      _stream(stream, device)), "ibp_attn_key_weights")
 
@@ -232,7 +237,7 @@ def ibp_attn_decode(q, k, v, table, lens, max_len, out, lse=None, weights=None, 
     need = 0
     if workspace is None:
         need = ibp_attn_decode_workspace(n, heads, kv_heads, dim, max_len, weights is not None)
-    at, size, held = _space(workspace, need, device)
+    at, size, held = _space(workspace, need, device, stream)
     check(lib().ibp_attn_decode(a, rq, pages, lens_at, max_len, ro, lse_at, weights_at, slots, at, size, _stream(stream, device)),
           "ibp_attn_decode")
 
@@ -264,7 +269,7 @@ def ibp_kv_evict(k, v, table, lens, max_len, budget, recent, next_positions, wei
     new_positions_at = _array(new_positions, "new_positions", torch.int32, device)
     a = ibp_attn(TYPES[k.dtype], kv_heads, kv_heads, dim, 1.0, 0)
     need = ibp_kv_evict_workspace(n, kv_heads, max_len, budget) if workspace is None else 0
-    at, size, held = _space(workspace, need, device)
+    at, size, held = _space(workspace, need, device, stream)
     check(lib().ibp_kv_evict(a, pages, lens_at, n, max_len, budget, recent, next_at, weights_at, positions_at,
                              weights.shape[2], new_weights_at, new_positions_at, new_weights.shape[2], new_lens_at, at,
                              size, _stream(stream, device)), "ibp_kv_evict")

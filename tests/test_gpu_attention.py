@@ -344,3 +344,23 @@ def test_binding_refuses(ibp):
     with pytest.raises(ibp.IbpError) as e:
         ibp.ibp_attn_key_weights(q, k, at, at, lse, w, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
     assert e.value.status == ibp.IBP_ENOMEM
+
+
+@pytest.mark.parametrize("as_handle", [False, True])
+def test_workspace_belongs_to_the_stream_of_the_call(ibp, as_handle):
+    """A workspace that the call takes itself, on a stream that is still busy, is not handed to the program's
+    current stream before the call's kernels are done with it."""
+    q, k = (torch.randn(n, h, 64, device="cuda").bfloat16() for n, h in ((100, 4), (2000, 2)))
+    starts = [torch.tensor([0, n], dtype=torch.int32, device="cuda") for n in (100, 2000)]
+    lse, weights, want = torch.zeros(4, 100, device="cuda"), *(torch.zeros(2, 2000, device="cuda") for _ in range(2))
+    need = ibp.ibp_attn_key_weights_workspace(4, 2, 2000, 1)
+    ibp.ibp_attn_key_weights(q, k, *starts, lse, want)
+    busy, side = torch.randn(4096, 4096, device="cuda"), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(10):
+            busy = busy @ busy * 1e-2
+    ibp.ibp_attn_key_weights(q, k, *starts, lse, weights, stream=side.cuda_stream if as_handle else side)
+    mine = torch.full((need,), 7, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    assert (mine == 7).all() and torch.equal(weights, want)
