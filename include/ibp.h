@@ -435,7 +435,7 @@ typedef struct {
  * strides (elements, multiples of 8), so that pages of [token][head] order serve too, and
  * which pages a sequence has: slot i of sequence s is token i % page_tokens of page
  * d_table[s * table_pages + i / page_tokens]. A slot whose page id is outside [0, n_pages)
- * counts as absent. */
+ * counts as absent; an empty pool (n_pages 0) holds no tokens, whatever the lengths say. */
 typedef struct {
     void *keys, *values;
     uint64_t n_pages;

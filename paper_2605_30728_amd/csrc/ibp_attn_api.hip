@@ -187,7 +187,7 @@ ibp_status evict_impl(const ibp_attn *a, const ibp_pages *pages, const int32_t *
     e.lens = d_lens;
     e.next = d_next;
     e.n_seqs = n_seqs;
-    e.max_len = max_len;
+    e.max_len = e.pg.n_pages ? max_len : 0;          // an empty pool holds no tokens
     e.budget = budget;
     e.recent = recent;
     e.weights = d_weights;

@@ -298,6 +298,20 @@ def test_evict_layout_and_positions_beyond(ibp):
     check_evict(c, weights, positions, nxt, 32, 32, (k.cpu(), v.cpu(), new_w.cpu(), new_p.cpu(), new_lens.cpu()))
 
 
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("n,budget", [(40, 39), (400, 200)])
+def test_evict_from_an_empty_pool(ibp, n, budget, in_place):
+    """A pool without pages holds no tokens: nothing is moved, new lengths are 0 and the rest stays."""
+    k, v = (torch.empty(0, 2, 16, 64, dtype=BF16, device="cuda") for _ in range(2))
+    table = torch.zeros(1, -(-n // 16), dtype=torch.int32, device="cuda")
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    weights, positions = torch.rand(1, 2, n, device="cuda"), torch.arange(n, dtype=torch.int32, device="cuda").repeat(1, 2, 1)
+    new_w, new_p = torch.full((1, 2, budget), 7.0, device="cuda"), torch.full((1, 2, budget), 7, dtype=torch.int32, device="cuda")
+    new_lens = lens if in_place else torch.full_like(lens, 7)
+    ibp.ibp_kv_evict(k, v, table, lens, n, budget, 3, lens.clone(), weights, positions, new_w, new_p, new_lens)
+    assert new_lens.tolist() == [0] and bool((new_w == 7).all()) and bool((new_p == 7).all())
+
+
 def test_decode_then_evict_in_a_graph(ibp):
     """A serving step captured into a graph and replayed with the program's own work between: every replay
     equals the same calls made one by one."""
