@@ -144,6 +144,13 @@ def _space(workspace, need, device, stream):
     return workspace.data_ptr(), workspace.numel(), workspace
 
 
+def _count(x, what):
+    """A number that the library takes in 32 bits, which ctypes would cut without a word."""
+    if not 0 <= x < 1 << 32:
+        raise ValueError(f"{what} must be from 0 to 2^32 - 1, not {x}")
+    return x
+
+
 def _stream(stream, device):
     if stream is None:       # the current stream's handle, without a Stream object around it
         return torch._C._cuda_getCurrentRawStream(device)
@@ -152,7 +159,8 @@ def _stream(stream, device):
 
 def ibp_attn_prompt_workspace(q_heads, head_dim, q_rows, k_rows, n_seqs):
     out = _u64(0)
-    check(lib().ibp_attn_prompt_workspace(q_heads, head_dim, q_rows, k_rows, n_seqs, out), "ibp_attn_prompt_workspace")
+    check(lib().ibp_attn_prompt_workspace(_count(q_heads, "q_heads"), _count(head_dim, "head_dim"), _count(q_rows, "q_rows"),
+                                          _count(k_rows, "k_rows"), _count(n_seqs, "n_seqs"), out), "ibp_attn_prompt_workspace")
     return out.value
 
 
@@ -179,7 +187,8 @@ def ibp_attn_prompt(q, k, v, q_starts, k_starts, out, lse=None, causal=True, sca
 
 def ibp_attn_key_weights_workspace(q_heads, kv_heads, k_rows, n_seqs=1):
     out = _u64(0)
-    check(lib().ibp_attn_key_weights_workspace(q_heads, kv_heads, k_rows, n_seqs, out), "ibp_attn_key_weights_workspace")
+    check(lib().ibp_attn_key_weights_workspace(_count(q_heads, "q_heads"), _count(kv_heads, "kv_heads"), _count(k_rows, "k_rows"),
+                                               _count(n_seqs, "n_seqs"), out), "ibp_attn_key_weights_workspace")
     return out.value
 
 
@@ -205,7 +214,8 @@ def ibp_attn_key_weights(q, k, q_starts, k_starts, lse, weights, causal=True, sc
 
 def ibp_attn_decode_workspace(n_seqs, q_heads, kv_heads, head_dim, max_len, weights):
     out = _u64(0)
-    check(lib().ibp_attn_decode_workspace(n_seqs, q_heads, kv_heads, head_dim, max_len, int(bool(weights)), out),
+    check(lib().ibp_attn_decode_workspace(_count(n_seqs, "n_seqs"), _count(q_heads, "q_heads"), _count(kv_heads, "kv_heads"),
+                                          _count(head_dim, "head_dim"), _count(max_len, "max_len"), int(bool(weights)), out),
           "ibp_attn_decode_workspace")
     return out.value
 
@@ -238,13 +248,14 @@ def ibp_attn_decode(q, k, v, table, lens, max_len, out, lse=None, weights=None, 
     if workspace is None:
         need = ibp_attn_decode_workspace(n, heads, kv_heads, dim, max_len, weights is not None)
     at, size, held = _space(workspace, need, device, stream)
-    check(lib().ibp_attn_decode(a, rq, pages, lens_at, max_len, ro, lse_at, weights_at, slots, at, size, _stream(stream, device)),
-          "ibp_attn_decode")
+    check(lib().ibp_attn_decode(a, rq, pages, lens_at, _count(max_len, "max_len"), ro, lse_at, weights_at, slots, at, size,
+                                _stream(stream, device)), "ibp_attn_decode")
 
 
 def ibp_kv_evict_workspace(n_seqs, kv_heads, max_len, budget):
     out = _u64(0)
-    check(lib().ibp_kv_evict_workspace(n_seqs, kv_heads, max_len, budget, out), "ibp_kv_evict_workspace")
+    check(lib().ibp_kv_evict_workspace(_count(n_seqs, "n_seqs"), _count(kv_heads, "kv_heads"), _count(max_len, "max_len"),
+                                       _count(budget, "budget"), out), "ibp_kv_evict_workspace")
     return out.value
 
 
@@ -270,6 +281,7 @@ def ibp_kv_evict(k, v, table, lens, max_len, budget, recent, next_positions, wei
     a = ibp_attn(TYPES[k.dtype], kv_heads, kv_heads, dim, 1.0, 0)
     need = ibp_kv_evict_workspace(n, kv_heads, max_len, budget) if workspace is None else 0
     at, size, held = _space(workspace, need, device, stream)
-    check(lib().ibp_kv_evict(a, pages, lens_at, n, max_len, budget, recent, next_at, weights_at, positions_at,
-                             weights.shape[2], new_weights_at, new_positions_at, new_weights.shape[2], new_lens_at, at,
-                             size, _stream(stream, device)), "ibp_kv_evict")
+    check(lib().ibp_kv_evict(a, pages, lens_at, n, _count(max_len, "max_len"), _count(budget, "budget"),
+                             _count(recent, "recent"), next_at, weights_at, positions_at, weights.shape[2], new_weights_at,
+                             new_positions_at, new_weights.shape[2], new_lens_at, at, size, _stream(stream, device)),
+          "ibp_kv_evict")

@@ -147,3 +147,15 @@ def test_binding_refuses_host_tensors():
         ibp.ibp_attn_prompt(q, q, q, starts, starts, q)
     with pytest.raises(TypeError):
         ibp.ibp_kv_evict(q[None], q[None], starts[None], starts[:1], 4, 2, 1, starts[:1], q, q, q, q, starts[:1])
+
+
+@pytest.mark.parametrize("call,good", [("ibp_attn_prompt_workspace", (4, 64, 100, 200, 1)), ("ibp_attn_key_weights_workspace", (4, 2, 100, 1)),
+                                       ("ibp_attn_decode_workspace", (2, 4, 2, 64, 300)), ("ibp_kv_evict_workspace", (2, 2, 300, 100))])
+def test_counts_of_more_than_32_bits_are_refused(call, good):
+    """Not taken as what their low 32 bits say."""
+    more = (True,) if call == "ibp_attn_decode_workspace" else ()
+    assert getattr(ibp, call)(*good, *more) >= 0
+    for i, x in enumerate(good):
+        for bad in (x + (1 << 32), -1):
+            with pytest.raises(ValueError):
+                getattr(ibp, call)(*good[:i], bad, *good[i + 1:], *more)
