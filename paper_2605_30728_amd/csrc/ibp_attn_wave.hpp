@@ -168,11 +168,9 @@ __device__ __forceinline__ void load_to_lds(Rsrc r, uint8_t *to, uint32_t offset
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (IBP_LDS(void) *)to, 16, (int)offset, 0, 0, 0);
 }
 
-// Waits for this wave's loads into LDS, all but the last `PENDING` that it issued, and for its reads
-// of LDS, then for the other waves.
-template <int PENDING = 0>
+// Waits for this wave's loads into LDS and for its reads of LDS, then for the other waves.
 __device__ __forceinline__ void tiles_loaded() {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(PENDING) : "memory");
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }

@@ -7,7 +7,7 @@
 // Bound by the matrix and the vector unit at once: of the pairs of a causal prompt each costs DIM multiply-adds, a
 // subtraction, an exponential and an addition, and nothing of that size is written. 64 keys a wave, since every
 // row fragment read from LDS then feeds two matrix instructions (with 32 keys LDS is as busy as they are);
-// rows reach LDS by direct loads two tiles ahead. 8,192 rows of 32 heads of 128 in bf16: 350 us with the sum
+// rows reach LDS by direct loads, issued a tile before the one that reads them. 8,192 rows of 32 heads of 128 in bf16: 350 us with the sum
 // over heads, 786 TFLOP/s of the pairs that count.
 #include "ibp_attn.hpp"
 #include "ibp_attn_wave.hpp"
@@ -191,7 +191,7 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_key_we
             }
             step<T, DIM>(qn, 0, k, s1, s0, lse_tile[here] + 32, sum, a.scale_log2);
             put_lse(free, next_lse);
-            tiles_loaded<kLoads>();                          // (the tile after the next is still on its way)
+            tiles_loaded();                                  // (the next tile's second step reads tile n + 2, every wave's share)
             const int old = here;
             here = then;
             then = free;

@@ -287,6 +287,20 @@ def test_key_weights_sum_to_the_rows(ibp):
     assert torch.allclose(w.double().sum(1), torch.full((2,), 4000.0, dtype=torch.float64), rtol=1e-5)
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("kind,heads,kv_heads,dim", [(BF16, 4, 2, 128), (F16, 3, 1, 64), (BF16, 1, 1, 96), (F16, 2, 1, 256)])
+def test_key_weights_many_tiles_of_rows(ibp, kind, heads, kv_heads, dim, causal):
+    """Blocks that stream many tiles of rows past their keys, several waves each loading a share of a tile: every
+    tile counts once, the same every time."""
+    lens = [2100], [300]
+    q, k, v = inputs(kind, heads, kv_heads, dim, *lens, seed=29)
+    _, lse = run_prompt(ibp, q, k, v, *lens, causal=causal)
+    w = run_weights(ibp, q, k, *lens, lse, causal=causal)
+    check_weights(q, k, *lens, lse, w, causal=causal)
+    for _ in range(8):
+        assert torch.equal(run_weights(ibp, q, k, *lens, lse, causal=causal), w)
+
+
 def test_key_weights_ignore_what_does_not_count(ibp):
     """A NaN row counts only for the keys it sees, a NaN key only for itself, a row without an lse not at all."""
     lens = [150], [150]
