@@ -70,7 +70,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_attn_decode(DecodeArgs a) {
     const uint32_t kv = hb / a.head_blocks, head0 = kv * a.group + hb % a.head_blocks * 16;
     const int heads = min((int)((kv + 1) * a.group - head0), 16);
     const int len = uniform(slots_of(a, seq));
-    const int from = split * a.split_tokens, to = min(len, from + (int)a.split_tokens);
+    const int from = split * a.split_tokens, to = from < len ? from + min(len - from, (int)a.split_tokens) : from;
     if (from >= to && !(split == 0)) return;
 
     Frag q[KS];

@@ -186,6 +186,23 @@ def test_decode_offsets_past_32_bits(ibp):
     assert torch.equal(out, want) and torch.equal(lse, want_lse)
 
 
+def test_decode_as_many_slots_as_there_can_be(ibp):
+    """2^31 - 256 slots, the most that a call takes, all of them one row (strides of 0): every slot weighs the
+    same, so lse = x + ln n and out is the value, to the bit; a split left out would show as ln of what is left
+    of n, 2e-3 less."""
+    n, page = (1 << 31) - 256, 1 << 24
+    q, row = (torch.randn(1, 1, 8, generator=torch.Generator().manual_seed(x)).to(BF16).cuda() for x in (1, 2))
+    value = torch.tensor([1.0, -2.0, 0.5, 4.0, -0.25, 8.0, 1.0, -1.0], dtype=BF16, device="cuda").view(1, 1, 8)
+    k, v = (x.unsqueeze(2).expand(1, 1, page, 8) for x in (row, value))
+    table, lens = torch.zeros(1, 128, dtype=torch.int32, device="cuda"), torch.tensor([n], dtype=torch.int32, device="cuda")
+    out, lse = torch.zeros_like(q), torch.zeros(1, 1, device="cuda")
+    ibp.ibp_attn_decode(q, k, v, table, lens, n, out, lse)
+    x = (q.double() @ row.double().transpose(1, 2)).item() * 8 ** -0.5
+    want = x + torch.log(torch.tensor(float(n), dtype=torch.float64)).item()
+    assert torch.equal(out, value)
+    assert abs(lse.item() - want) <= 2.0 ** -20 * (abs(want) + abs(x))      # a logarithm and two sums in 32 bits
+
+
 # ---------------------------------------------------------------- eviction
 
 def run_evict(ibp, c, weights, positions, next_positions, budget, recent, in_place=False, max_len=None):
