@@ -391,7 +391,7 @@ DecodePlan plan_decode(uint32_t n_seqs, uint32_t q_heads, uint32_t kv_heads, uin
     const uint64_t rows = std::max<uint64_t>((uint64_t)n_seqs * kv_heads * p.head_blocks, 1), len = std::max<uint64_t>(max_len, 1);
     uint64_t t = n_seqs > 1 ? std::min<uint64_t>((len * rows + 1023) / 1024, 768) : (len * rows + 511) / 512;
     t = std::max<uint64_t>(t, (len + kMaxSplits - 1) / kMaxSplits);
-    t = std::max<uint64_t>((t + 127) / 128 * 128, 128);
+    t = std::max<uint64_t>((std::min(t, len) + 127) / 128 * 128, 128);   // (below 2^31, however many heads there are)
     p.split_tokens = (uint32_t)t;
     p.splits = (uint32_t)((len + t - 1) / t);
     const uint64_t parts = (uint64_t)n_seqs * q_heads * p.splits;

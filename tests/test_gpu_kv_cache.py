@@ -203,6 +203,24 @@ def test_decode_as_many_slots_as_there_can_be(ibp):
     assert abs(lse.item() - want) <= 2.0 ** -20 * (abs(want) + abs(x))      # a logarithm and two sums in 32 bits
 
 
+@pytest.mark.parametrize("heads", [64, 1024])
+def test_decode_of_many_heads_under_a_wide_bound(ibp, heads):
+    """max_len is only a bound: with as large a one as there is, and so many KV heads that each block could take more
+    slots than 32 bits count, a short cache is read as it is."""
+    n, page, most = 100, 128, (1 << 31) - 256
+    g = torch.Generator().manual_seed(heads)
+    q, k, v = (torch.randn(x, heads, 64, generator=g).to(BF16) for x in (1, page, page))
+    pool = [x.cuda()[None].transpose(1, 2) for x in (k, v)]              # one page
+    k, v = k[:n], v[:n]
+    table, lens = torch.zeros(1, 1 << 24, dtype=torch.int32, device="cuda"), torch.tensor([n], dtype=torch.int32, device="cuda")
+    out, lse = torch.zeros(1, heads, 64, dtype=BF16, device="cuda"), torch.zeros(1, heads, device="cuda")
+    ibp.ibp_attn_decode(q.cuda(), *pool, table, lens, most, out, lse)
+    out, lse = out.cpu(), lse.cpu()
+    for h in range(heads):
+        o, x, o_tol, x_tol = attend(q[:, h], k[:, h], v[:, h], 64 ** -0.5, torch.ones(1, n, dtype=torch.bool))
+        assert abs(lse[0, h].double() - x[0]) <= x_tol[0] and ((out[0, h].double() - o[0]).abs() <= o_tol[0]).all()
+
+
 # ---------------------------------------------------------------- eviction
 
 def run_evict(ibp, c, weights, positions, next_positions, budget, recent, in_place=False, max_len=None):
