@@ -508,7 +508,7 @@ ibp_status ibp_attn_decode(const ibp_attn *a, const ibp_rows *q, const ibp_pages
  * [new_stride] and may be the same arrays (of the same stride); of them the first m slots are
  * written. d_new_lens[s] = m may be d_lens. Pages must not be shared between sequences. Of
  * `a` the type, kv_heads and head_dim are used (a valid q_heads and scale still given).
- * recent <= budget, budget >= 1.
+ * recent <= budget, budget >= 1, max_len at most 2^31 - 2^24.
  */
 ibp_status ibp_kv_evict_workspace(uint32_t n_seqs, uint32_t kv_heads, uint32_t max_len, uint32_t budget,
                                   uint64_t *bytes);

@@ -11,6 +11,7 @@ namespace ibp {
 namespace {
 
 constexpr uint64_t kMaxRows = 0x7fffff00ull;      // rows and slots are counted in 31 bits
+constexpr uint64_t kMaxEvictSlots = 0x7f000000ull;   // so that a block's last rounds and two numbers per move fit 31 bits
 constexpr uint64_t kMaxRowStride = 1ull << 23;    // elements: 64 rows stay within 2^31 bytes
 
 bool aligned(const void *p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
@@ -172,6 +173,7 @@ ibp_status evict_impl(const ibp_attn *a, const ibp_pages *pages, const int32_t *
     IBP_TRY(take_shape(a, s));
     IBP_TRY(take_pages(pages, max_len, e.pg));
     IBP_TRY(check_paged(n_seqs, s.kv_heads, d_lens));
+    if (max_len > kMaxEvictSlots) return fail(IBP_EINVAL, "max_len is too large for an eviction");
     if (budget == 0 || budget > kMaxRows) return fail(IBP_EINVAL, "budget must be at least 1");
     if (recent > budget) return fail(IBP_EINVAL, "more recent positions than the budget");
     if (n_seqs == 0) return IBP_OK;
@@ -270,7 +272,7 @@ ibp_status ibp_attn_decode(const ibp_attn *a, const ibp_rows *q, const ibp_pages
 ibp_status ibp_kv_evict_workspace(uint32_t n_seqs, uint32_t kv_heads, uint32_t max_len, uint32_t budget, uint64_t *bytes) {
     clear_error();
     if (!bytes) return fail(IBP_EINVAL, "bytes is null");
-    if (kv_heads == 0 || max_len > kMaxRows || budget == 0 || budget > kMaxRows || (uint64_t)n_seqs * kv_heads > attn::kMaxGrid)
+    if (kv_heads == 0 || max_len > kMaxEvictSlots || budget == 0 || budget > kMaxRows || (uint64_t)n_seqs * kv_heads > attn::kMaxGrid)
         return fail(IBP_EINVAL, "bad sizes");
     *bytes = attn::evict_workspace(n_seqs, kv_heads, max_len, budget);
     return IBP_OK;

@@ -141,6 +141,17 @@ def test_evict_refuses():
     assert status("ibp_kv_evict_workspace", 1, 2, 20, 0, need) == ibp.IBP_EINVAL
 
 
+def test_evict_takes_no_more_slots_than_it_counts():
+    """A block's threads go a round beyond the last slot, and a list of moves has two numbers for each: both have
+    to fit 31 bits."""
+    most, need = (1 << 31) - (1 << 24), ctypes.c_uint64(0)
+    assert status("ibp_kv_evict_workspace", 1, 2, most, 5, need) == ibp.IBP_OK
+    for beyond in (most + 1, (1 << 31) - 256):
+        assert status("ibp_kv_evict_workspace", 1, 2, beyond, 5, need) == ibp.IBP_EINVAL
+        g = pages(page_tokens=1 << 24, table_pages=128)
+        assert status("ibp_kv_evict", attn(), g, A, 1, beyond, 5, 1, A, A, A, beyond, A + 4096, A + 4096, 20, A, A, 1 << 30, None) == ibp.IBP_EINVAL
+
+
 def test_binding_refuses_host_tensors():
     q, starts = torch.zeros(4, 2, 64, dtype=torch.bfloat16), torch.tensor([0, 4], dtype=torch.int32)
     with pytest.raises(TypeError):
