@@ -488,7 +488,9 @@ ibp_status ibp_attn_key_weights(const ibp_attn *a, const ibp_rows *q, const ibp_
  * cache already). max_len bounds the lengths (a longer one is taken as max_len; IBP_ERANGE
  * when the table holds fewer slots). d_lse ([sequences][q_heads]) may be null. d_weights, if
  * not null, is [sequences][kv_heads][weights_stride]: the sum over the query heads of a KV
- * head of exp(x - lse) is added to each slot's.
+ * head of exp(x - lse) is added to each slot's. The workspace of n_seqs sequences and max_len
+ * is enough for every call of the same heads with fewer sequences or a smaller max_len: a
+ * program needs one, of its largest sizes.
  */
 ibp_status ibp_attn_decode_workspace(uint32_t n_seqs, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim,
                                      uint32_t max_len, int weights, uint64_t *bytes);

@@ -71,6 +71,8 @@ struct DecodePlan {
 };
 DecodePlan plan_decode(uint32_t n_seqs, uint32_t q_heads, uint32_t kv_heads, uint32_t dim, uint32_t max_len,
                        bool weights);
+// Enough for the plan of this and of every smaller call (fewer sequences, a smaller max_len).
+uint64_t decode_workspace(uint32_t n_seqs, uint32_t q_heads, uint32_t kv_heads, uint32_t dim, uint32_t max_len, bool weights);
 
 hipError_t launch_decode(const Shape &a, const Rows &q, const Pages &pg, const int32_t *lens, uint32_t n_seqs,
                          uint32_t max_len, const Rows &out, float *lse, float *weights, uint64_t weights_stride,

@@ -255,7 +255,7 @@ ibp_status ibp_attn_decode_workspace(uint32_t n_seqs, uint32_t q_heads, uint32_t
     if (kv_heads == 0 || q_heads == 0 || q_heads % kv_heads || q_heads > 65536 || head_dim == 0 || head_dim % 8 ||
         head_dim > 256 || max_len > kMaxRows || (uint64_t)n_seqs * kv_heads > attn::kMaxGrid)
         return fail(IBP_EINVAL, "bad sizes");
-    *bytes = n_seqs ? attn::plan_decode(n_seqs, q_heads, kv_heads, head_dim, max_len, weights != 0).bytes : 0;
+    *bytes = n_seqs ? attn::decode_workspace(n_seqs, q_heads, kv_heads, head_dim, max_len, weights != 0) : 0;
     return IBP_OK;
 }
 

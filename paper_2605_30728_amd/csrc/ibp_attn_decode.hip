@@ -402,6 +402,18 @@ DecodePlan plan_decode(uint32_t n_seqs, uint32_t q_heads, uint32_t kv_heads, uin
     return p;
 }
 
+// What plan_decode needs at most for up to n_seqs sequences of up to max_len slots. Fewer slots can need more: a
+// split's length goes in steps of 128, so 8,192 slots of a sequence of 8 KV heads make 64 splits and 8,193
+// slots 33. By plan_decode's rule a sequence has a split for every 128 slots at most, and no more than both 768
+// slots each and 1,024 blocks among all sequences (each rounded up) come to; this grows with both sizes.
+uint64_t decode_workspace(uint32_t n_seqs, uint32_t q_heads, uint32_t kv_heads, uint32_t dim, uint32_t max_len, bool weights) {
+    const uint64_t n = n_seqs, len = std::max<uint64_t>(max_len, 1), blocks = (uint64_t)kv_heads * ((q_heads / kv_heads + 15) / 16);
+    const uint64_t splits = std::min(n * std::min<uint64_t>((len + 127) / 128, kMaxSplits),
+                                     std::max((1024 + blocks - 1) / blocks + n, n * ((len + 767) / 768)));
+    return up256(splits * q_heads * 8) + (len > 128 ? up256(splits * q_heads * dim * 4) : 0) +
+           (weights ? up256(n * q_heads * ((max_len + 31ull) / 32 * 32) * 4) : 0);
+}
+
 hipError_t launch_decode(const Shape &s, const Rows &q, const Pages &pg, const int32_t *lens, uint32_t n_seqs,
                          uint32_t max_len, const Rows &out, float *lse, float *weights, uint64_t weights_stride,
                          const DecodePlan &plan, uint8_t *workspace, hipStream_t stream) {

@@ -152,6 +152,24 @@ def test_evict_takes_no_more_slots_than_it_counts():
         assert status("ibp_kv_evict", attn(), g, A, 1, beyond, 5, 1, A, A, A, beyond, A + 4096, A + 4096, 20, A, A, 1 << 30, None) == ibp.IBP_EINVAL
 
 
+def growing(call, sizes):
+    """Whether the workspace call's answers never fall along the sizes."""
+    need = [call(*x) for x in sizes]
+    return all(a <= b for a, b in zip(need, need[1:]))
+
+
+@pytest.mark.parametrize("weights", [False, True])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(32, 8, 128), (8, 1, 256), (6, 2, 64), (16, 16, 80), (600, 600, 8), (64, 1, 128)])
+def test_decode_workspace_is_enough_for_smaller_calls(heads, kv_heads, dim, weights):
+    """A program takes one workspace, of its most sequences and longest cache."""
+    lens = sorted({128 * n + d for n in range(1, 140) for d in (-1, 0, 1)} | {1 << n for n in range(31)} | {3 << n for n in range(29)} | {0})
+    call = lambda n, m: ibp.ibp_attn_decode_workspace(n, heads, kv_heads, dim, m, weights)  # noqa: E731
+    for n in (1, 2, 3, 5, 24, 64):
+        assert growing(call, [(n, m) for m in lens])
+    for m in (100, 513, 5500, 8193, 131071):
+        assert growing(call, [(n, m) for n in range(80)])
+
+
 def test_binding_refuses_host_tensors():
     q, starts = torch.zeros(4, 2, 64, dtype=torch.bfloat16), torch.tensor([0, 4], dtype=torch.int32)
     with pytest.raises(TypeError):

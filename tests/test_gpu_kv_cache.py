@@ -75,6 +75,14 @@ def check_decode(c, q, out, lse, before=None, after=None, slots=None):
                 assert torch.equal(after[b, g, rest], before[b, g, rest])
 
 
+def check_decode_head(c, q, out, lse):
+    """The first query head of the sequences that are there."""
+    for b in range(out.shape[0]):
+        k, v = (c.rows(x, b, 0, range(c.lens[b])) for x in (c.k, c.v))
+        o, x, o_tol, x_tol = attend(q[b, :1].cpu(), k, v, c.dim ** -0.5, torch.ones(1, c.lens[b], dtype=torch.bool))
+        assert abs(lse[b, 0].cpu().double() - x[0]) <= x_tol[0] and ((out[b, 0].cpu().double() - o[0]).abs() <= o_tol[0]).all()
+
+
 def queries(c, heads, kind, seed=1):
     return torch.randn(len(c.lens), heads, c.dim, generator=torch.Generator().manual_seed(seed)).to(kind)
 
@@ -219,6 +227,28 @@ def test_decode_of_many_heads_under_a_wide_bound(ibp, heads):
     for h in range(heads):
         o, x, o_tol, x_tol = attend(q[:, h], k[:, h], v[:, h], 64 ** -0.5, torch.ones(1, n, dtype=torch.bool))
         assert abs(lse[0, h].double() - x[0]) <= x_tol[0] and ((out[0, h].double() - o[0]).abs() <= o_tol[0]).all()
+
+
+def test_decode_with_one_workspace_for_all_sizes(ibp):
+    """The workspace of the most sequences and the largest max_len serves every smaller call, on both sides of the
+    sizes at which the number of splits falls, with the result that a workspace of its own gives."""
+    c = Cache(BF16, 8, 64, [300, 1, 170], 16, seed=9)
+    q = queries(c, 8, BF16).cuda()
+    k, v = c.k.cuda(), c.v.cuda()
+    table = torch.cat([c.table, torch.zeros(3, 600, dtype=torch.int32)], 1).cuda()
+    lens = torch.tensor(c.lens, dtype=torch.int32, device="cuda")
+    out, lse = torch.zeros_like(q), torch.zeros(3, 8, device="cuda")
+    for weights in (False, True):
+        space = torch.empty(ibp.ibp_attn_decode_workspace(3, 8, 8, 64, 9000, weights), dtype=torch.uint8, device="cuda")
+        for n in (1, 2, 3):
+            for m in (300, 384, 385, 4095, 5461, 5462, 8191, 8192, 8193, 8999, 9000):
+                results = []
+                for w in (space, None):
+                    total = torch.zeros(n, 8, m, device="cuda") if weights else None
+                    ibp.ibp_attn_decode(q[:n], k, v, table[:n], lens[:n], m, out[:n], lse[:n], weights=total, workspace=w)
+                    results.append((out[:n].clone(), lse[:n].clone(), total))
+                assert all(a is None or torch.equal(a, b) for a, b in zip(*results))
+                check_decode_head(c, q, *results[0][:2])
 
 
 # ---------------------------------------------------------------- eviction

@@ -71,3 +71,13 @@ def test_every_result(example, history, turn, budget):
             assert ((weights[g, k0:k0 + m].double() - total).abs() <= total_tol + 2.0 ** -23 * group * total).all()
     assert len(tokens) == 5 and cache.next.tolist() == [n + t + 5 for n, t in zip(history, turn)]
     assert cache.lens.tolist() == [min(n + t + 5, budget) for n, t in zip(history, turn)]
+
+
+def test_one_workspace_serves_a_cache_at_its_budget(example):
+    """The loop's decode workspace is that of the whole cache, its calls are shorter: 5,401 slots of 5,500, between
+    which the number of splits falls."""
+    tokens = []
+    _, cache, _ = example.run((5400, 0, 0), (100, 1, 1), 2, 32, 8, 128, 5400, 64, 32,
+                              on_token=lambda q, cache, out, before: tokens.append((cache.lens.tolist(), bool(torch.isfinite(out.float()).all()))))
+    assert tokens == [([5401, 2, 2], True), ([5401, 3, 3], True)]
+    assert cache.lens.tolist() == [5400, 3, 3] and cache.next.tolist() == [5502, 3, 3]
