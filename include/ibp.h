@@ -456,8 +456,10 @@ typedef struct {
  * A row that sees no key, or only scores of -inf, gives zeros and an lse of -inf. What a row
  * does not see has no effect on it, infinities and NaN included. d_lse ([q_heads][q rows])
  * may be null. Rows of q outside all sequences leave out and d_lse as they are. Few rows
- * against many keys are split along the keys and joined; their parts are in the workspace
- * (0 bytes for other sizes, and then it may be null).
+ * against many keys are split along the keys and joined; their parts are in the workspace,
+ * which other calls do not use. The workspace of q_rows, k_rows and n_seqs is enough for every
+ * call of the same heads with no more rows and no fewer sequences (so n_seqs = 1 serves any
+ * number); where it has 0 bytes, it may be null.
  */
 ibp_status ibp_attn_prompt_workspace(uint32_t q_heads, uint32_t head_dim, uint64_t q_rows, uint64_t k_rows,
                                      uint32_t n_seqs, uint64_t *bytes);

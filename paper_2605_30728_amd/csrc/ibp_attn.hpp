@@ -35,7 +35,9 @@ struct Packed {
 
 hipError_t launch_prompt(const Shape &a, const Rows &q, const Rows &k, const Rows &v, const Packed &p, const Rows &out,
                          float *lse, uint8_t *workspace, hipStream_t stream);
-// (none where the tiles fill the chip by themselves)
+// What a call needs (nothing where the tiles fill the chip by themselves), and what is enough for it and for every
+// call of fewer rows.
+uint64_t prompt_needs(uint32_t q_heads, uint32_t dim, uint64_t q_rows, uint64_t k_rows, uint32_t n_seqs);
 uint64_t prompt_workspace(uint32_t q_heads, uint32_t dim, uint64_t q_rows, uint64_t k_rows, uint32_t n_seqs);
 
 // partial: the workspace (unused, may be null, where it has 0 bytes).

@@ -120,7 +120,7 @@ ibp_status prompt_impl(const ibp_attn *a, const ibp_rows *q, const ibp_rows *k, 
     if (v->rows != k->rows) return fail(IBP_EINVAL, "k and v must have the same rows");
     if (out->rows < q->rows) return fail(IBP_ENOMEM, "out has fewer rows than q");
     IBP_TRY(take_starts(d_q_starts, d_k_starts, n_seqs, q->rows, k->rows, p));
-    IBP_TRY(take_workspace(workspace, workspace_bytes, attn::prompt_workspace(s.q_heads, s.dim, q->rows, k->rows, n_seqs)));
+    IBP_TRY(take_workspace(workspace, workspace_bytes, attn::prompt_needs(s.q_heads, s.dim, q->rows, k->rows, n_seqs)));
     return launched(attn::launch_prompt(s, rq, rk, rv, p, ro, d_lse, static_cast<uint8_t *>(workspace),
                                         static_cast<hipStream_t>(stream)));
 }

@@ -431,21 +431,39 @@ hipError_t prompt_of(const PromptArgs &a, uint32_t blocks, hipStream_t stream) {
 // What the tiles of all sequences come to at most.
 uint64_t tiles_of(uint64_t q_rows, uint64_t n_seqs) { return q_rows / kBlockRows + n_seqs; }
 
-// Blocks that share a tile's keys: as many as leave none of the chip's 512 places empty, each with at least 512 keys of a
+constexpr uint64_t kPlaces = 512;        // blocks that the chip holds at once
+
+// Blocks that share a tile's keys: as many as leave none of the chip's places empty, each with at least 512 keys of a
 // sequence of average length (1,000 rows of 16 heads of 64 against 9,001 keys: 59 us, in one block each 125).
 uint32_t splits_of(uint32_t q_heads, uint64_t q_rows, uint64_t k_rows, uint64_t n_seqs) {
     const uint64_t blocks = tiles_of(q_rows, n_seqs) * q_heads;
     if (n_seqs == 0 || blocks == 0) return 1;
-    return (uint32_t)std::max<uint64_t>(std::min<uint64_t>({(uint64_t)kMaxSplits, 512 / blocks, k_rows / n_seqs / 512}), 1);
+    return (uint32_t)std::max<uint64_t>(std::min<uint64_t>({(uint64_t)kMaxSplits, kPlaces / blocks, k_rows / n_seqs / 512}), 1);
 }
 
 uint64_t up256(uint64_t x) { return (x + 255) / 256 * 256; }
 
+// Of a call: what its parts take (none where one block per tile does).
+uint64_t prompt_parts(uint32_t q_heads, uint32_t dim, uint64_t q_rows, uint64_t splits) {
+    const uint64_t parts = splits > 1 ? splits * q_heads * q_rows : 0;
+    return up256(parts * 8) + up256(parts * dim * 4);
+}
+
 }  // namespace
 
+uint64_t prompt_needs(uint32_t q_heads, uint32_t dim, uint64_t q_rows, uint64_t k_rows, uint32_t n_seqs) {
+    return prompt_parts(q_heads, dim, q_rows, splits_of(q_heads, q_rows, k_rows, n_seqs));
+}
+
+// Fewer rows make fewer blocks, which are split more: of every number of splits that the keys
+// allow, with the most rows that are split that often.
 uint64_t prompt_workspace(uint32_t q_heads, uint32_t dim, uint64_t q_rows, uint64_t k_rows, uint32_t n_seqs) {
-    const uint64_t splits = splits_of(q_heads, q_rows, k_rows, n_seqs), parts = splits * q_heads * q_rows;
-    return splits > 1 ? up256(parts * 8) + up256(parts * dim * 4) : 0;
+    uint64_t most = 0;
+    for (uint64_t splits = 2; n_seqs && splits <= std::min<uint64_t>(kMaxSplits, k_rows / n_seqs / 512); ++splits) {
+        const uint64_t tiles = kPlaces / splits / q_heads;
+        if (tiles >= n_seqs) most = std::max(most, prompt_parts(q_heads, dim, std::min(q_rows, (tiles - n_seqs + 1) * kBlockRows - 1), splits));
+    }
+    return most;
 }
 
 hipError_t launch_prompt(const Shape &s, const Rows &q, const Rows &k, const Rows &v, const Packed &p, const Rows &out,

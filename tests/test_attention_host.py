@@ -170,6 +170,20 @@ def test_decode_workspace_is_enough_for_smaller_calls(heads, kv_heads, dim, weig
         assert growing(call, [(n, m) for n in range(80)])
 
 
+@pytest.mark.parametrize("heads,dim", [(32, 128), (16, 64), (1, 256), (5, 80), (40, 128), (200, 8), (600, 64)])
+def test_prompt_workspace_is_enough_for_smaller_calls(heads, dim):
+    """Of fewer rows of queries or keys, or more sequences that they belong to: few rows are split more than many."""
+    rows = sorted({128 * n + d for n in range(1, 70) for d in (-1, 0, 1)} | {1, 8, 77, 8192, 20001, 1 << 20} | {0})
+    call = lambda q, k, n: ibp.ibp_attn_prompt_workspace(heads, dim, q, k, n)  # noqa: E731
+    for n in (1, 2, 3, 11):
+        for k in (512, 1024, 5000, 9001, 131072):
+            assert growing(call, [(q, k, n) for q in rows])
+        for q in (1, 128, 1000, 8192):
+            assert growing(call, [(q, k, n) for k in sorted({512 * n for n in range(20)} | {512 * n - 1 for n in range(1, 20)} | {1 << 20})])
+    for q in (1, 300, 4096):
+        assert growing(call, [(q, 9001, n) for n in range(20, 0, -1)])
+
+
 def test_binding_refuses_host_tensors():
     q, starts = torch.zeros(4, 2, 64, dtype=torch.bfloat16), torch.tensor([0, 4], dtype=torch.int32)
     with pytest.raises(TypeError):

@@ -115,6 +115,24 @@ def test_prompt_few_rows_many_keys(ibp, kind, heads, kv_heads, dim, causal):
         assert torch.allclose(bad.float(), out.float(), rtol=0.02, atol=0.02)
 
 
+def test_prompt_with_one_workspace_for_all_sizes(ibp):
+    """The workspace of the most rows and keys, as one sequence, serves every call of fewer, with the result that a
+    workspace of its own gives; what was refused before are the sizes that are split, after one that is not."""
+    heads, dim, most = 16, 64, (3000, 6000)
+    q, k, v = (x.cuda() for x in inputs(BF16, heads, 1, dim, [most[0]], [most[1]], seed=31))
+    space = torch.empty(ibp.ibp_attn_prompt_workspace(heads, dim, *most, 1), dtype=torch.uint8, device="cuda")
+    for q_lens, k_lens in ([3000], [6000]), ([1023], [6000]), ([1024], [6000]), ([77], [5000]), ([1], [1024]), ([500, 1, 300], [3000, 2, 2800]):
+        nq, nk = sum(q_lens), sum(k_lens)
+        results = []
+        for w in (space, None):
+            out, lse = torch.zeros_like(q[:nq]), torch.zeros(heads, nq, device="cuda")
+            ibp.ibp_attn_prompt(q[:nq], k[:nk], v[:nk], starts(q_lens).cuda(), starts(k_lens).cuda(), out, lse, workspace=w)
+            results.append((out, lse))
+        assert torch.equal(results[0][0], results[1][0]) and torch.equal(results[0][1], results[1][1])
+        if nq <= 100:
+            check_prompt(q[:nq].cpu(), k[:nk].cpu(), v[:nk].cpu(), q_lens, k_lens, results[0][0].cpu(), results[0][1].cpu())
+
+
 @pytest.mark.parametrize("dim", [64, 128, 256])
 def test_prompt_many_sequences(ibp, dim):
     """More sequences than a wave has lanes, empty ones among them."""
