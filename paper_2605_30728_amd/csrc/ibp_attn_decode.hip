@@ -9,8 +9,8 @@
 //
 // Bound by HBM: every slot's key and value are read once and used by the heads that share them (up to
 // 16 as the columns of one matrix product). They go to registers a chunk ahead of their use, the values on to
-// LDS, which turns them for the second product; the weights are rounded to the inputs' type for it, their sum is
-// of the unrounded ones. 131,071 slots of 8 heads of 128 in bf16: 100 us, 5.4 TB/s; 64 sequences of up to
+// LDS, which turns them for the second product; the weights are rounded to the inputs' type for it (float16's
+// lifted first, see lift_of), their sum is of the unrounded ones. 131,071 slots of 8 heads of 128 in bf16: 100 us, 5.4 TB/s; 64 sequences of up to
 // 8,192 slots with the slots' weights: 249 us, 4.5 TB/s of what the call has to move (the scores'
 // way through the workspace comes on top). Short caches are bound by two launches: 1,531 slots in 13 us.
 #include "ibp_attn.hpp"
@@ -92,7 +92,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_attn_decode(DecodeArgs a) {
 
     const float inf = __builtin_inff();
     const float c = a.scale_log2;
-    float m = -inf, l = 0.f;
+    float m = -inf, mc = 0.f, l = 0.f;      // reference, what exponents are relative to, sum
     f32x4 acc[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = f32x4{};
@@ -170,13 +170,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_attn_decode(DecodeArgs a) {
         top = max_halves(max_quarters(top));
         if (__any(top > m)) {
             const float next = fmaxf(m, top);
-            const float keep = m == -inf ? 0.f : exp2_fast((m - next) * c);
+            const float keep = keep_of<T>(m, next, c);
             l *= keep;
 #pragma unroll
             for (int d = 0; d < DT; ++d) acc[d] *= keep;
             m = next;
+            mc = base_of<T>(m, c);
         }
-        const float mc = m == -inf ? 0.f : m * c;
         u32x2 p[KT];
 #pragma unroll
         for (int j = 0; j < KT; ++j) {
@@ -202,7 +202,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_attn_decode(DecodeArgs a) {
     }
 
     // the block's waves joined: lane's column is a head, its registers dims quarter * 4 + i
-    l = sum_halves(sum_quarters(l));
+    const float unit = unit_of<T>(m, c);
+    l = sum_halves(sum_quarters(l)) * unit;
     if (quarter == 0) {
         stat[wave][0][col] = m;
         stat[wave][1][col] = l;
@@ -210,7 +211,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_attn_decode(DecodeArgs a) {
     __syncthreads();
     float *mine = reinterpret_cast<float *>(vt);
 #pragma unroll
-    for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4 *>(mine + col * (DIM + 4) + d * 16 + quarter * 4) = acc[d];
+    for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4 *>(mine + col * (DIM + 4) + d * 16 + quarter * 4) = acc[d] * unit;
     __syncthreads();
     const int h = threadIdx.x >> 4;          // 16 heads, 16 threads each
     if (h >= heads) return;

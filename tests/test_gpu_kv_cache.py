@@ -229,6 +229,58 @@ def test_decode_of_many_heads_under_a_wide_bound(ibp, heads):
         assert abs(lse[0, h].double() - x[0]) <= x_tol[0] and ((out[0, h].double() - o[0]).abs() <= o_tol[0]).all()
 
 
+@pytest.mark.parametrize("kind", [F16, BF16])
+@pytest.mark.parametrize("heads,dim,n,page", [(1, 64, 131071, 64), (64, 128, 9000, 32), (512, 64, 20000, 64), (512, 128, 6000, 32),
+                                              (512, 256, 6000, 32)])
+def test_decode_one_slot_above_many(ibp, kind, heads, dim, n, page):
+    """One slot takes nearly all of the weight and has a value of 0; what the others, at 2^-25 to 2^-30 of its weight,
+    add up to is the output. None of them may be lost, in the block of the one least of all (with many heads a
+    block has the whole cache): `attend`'s bound, with float16's spacing taken at the 2^12 by which its weights are
+    lifted before they are rounded."""
+    g = torch.Generator().manual_seed(n)
+    pages = -(-n // page)
+    k, v = torch.zeros(pages, 1, page, dim, dtype=kind), torch.zeros(pages, 1, page, dim, dtype=kind)
+    rows_k, rows_v = k.view(-1, dim), v.view(-1, dim)
+    rows_k[:, 1:] = torch.randn(rows_k.shape[0], dim - 1, generator=g).to(kind)       # (not seen by q)
+    rows_k[:, 0] = -(17.5 + 3.5 * torch.rand(rows_k.shape[0], generator=g)).to(kind)
+    rows_v[:] = (0.5 + torch.rand(rows_v.shape, generator=g)).to(kind)
+    at = n // 3
+    rows_k[at, 0], rows_v[at] = 0.0, 0.0
+    q = torch.zeros(1, 1, dim, dtype=kind)
+    q[0, 0, 0] = 1.0
+    out, lse = torch.zeros(1, heads, dim, dtype=kind, device="cuda"), torch.zeros(1, heads, device="cuda")
+    table, lens = torch.arange(pages, dtype=torch.int32, device="cuda")[None], torch.tensor([n], dtype=torch.int32, device="cuda")
+    ibp.ibp_attn_decode(q.cuda().expand(1, heads, dim), *(x.cuda().expand(-1, heads, -1, -1) for x in (k, v)), table, lens, n,
+                        out, lse, scale=1.0)
+    assert torch.equal(out, out[:, :1].expand_as(out)) and torch.equal(lse, lse[:, :1].expand_as(lse))
+    o, x, o_tol, x_tol = attend(q[:, 0], rows_k[:n], rows_v[:n], 1.0, torch.ones(1, n, dtype=torch.bool))
+    if kind == F16:
+        o_tol -= 2.0 ** -24 * (1 - 2.0 ** -12) * rows_v[:n].double().sum(0)
+    assert abs(lse.cpu()[0, 0].double() - x[0]) <= x_tol[0]
+    off = (out.cpu()[0, 0].double() - o[0]).abs()
+    assert (off <= o_tol[0]).all(), (off / o[0]).max()
+
+
+@pytest.mark.parametrize("falling", [False, True])
+@pytest.mark.parametrize("kind", [F16, BF16])
+def test_decode_scores_of_millions(ibp, kind, falling):
+    """Scores from 0 to 6.5 million in steps of thousands: the largest takes all, whatever the reference was before."""
+    n = 1024
+    k, v = (torch.randn(n // 16, 1, 16, 64, generator=torch.Generator().manual_seed(x)).to(kind) for x in (1, 2))
+    scores = torch.arange(n, dtype=torch.float32) * 64
+    k.view(n, 64)[:, 0] = (scores.flip(0) if falling else scores).to(kind)
+    q = torch.zeros(1, 1, 64, dtype=kind, device="cuda")
+    q[..., 0] = 1.0
+    out, lse = torch.zeros_like(q), torch.zeros(1, 1, device="cuda")
+    table, lens = torch.arange(n // 16, dtype=torch.int32, device="cuda")[None], torch.tensor([n], dtype=torch.int32, device="cuda")
+    ibp.ibp_attn_decode(q, k.cuda(), v.cuda(), table, lens, n, out, lse, scale=100.0)
+    top = k.view(n, 64)[:, 0].max()
+    best = (k.view(n, 64)[:, 0] == top).nonzero()[:, 0]                  # (bfloat16 has several of the largest)
+    want, tol = v.view(n, 64)[best].double().mean(0), 2.0 ** (-10 if kind == F16 else -7)
+    assert ((out[0, 0].cpu().double() - want).abs() <= tol * v.view(n, 64)[best].double().abs().mean(0) + 2.0 ** -24).all()
+    assert abs(lse.item() - top.item() * 100.0) <= 2.0 ** -21 * top.item() * 100.0 + len(best)
+
+
 def test_decode_with_one_workspace_for_all_sizes(ibp):
     """The workspace of the most sequences and the largest max_len serves every smaller call, on both sides of the
     sizes at which the number of splits falls, with the result that a workspace of its own gives."""
