@@ -9,8 +9,8 @@
 // exponential for every pair of a row and a key. Keys and values are read from HBM about once (the heads
 // that share them run on one XCD). A wave holds 32 rows' queries, weights and sums in registers, four waves share
 // the tiles of 64 keys (32 of wide heads) that LDS holds, two of K and two of V. The weights are rounded to the
-// inputs' type for the product with the values, as the matrix unit takes them; their sum is of the unrounded
-// ones. 8,192 rows of 32 heads of 128 in bf16, causal: 508 to 531 us, 1.04 to 1.08 PFLOP/s of the
+// inputs' type for the product with the values, as the matrix unit takes them (float16's lifted first, see lift_of);
+// their sum is of the unrounded ones. 8,192 rows of 32 heads of 128 in bf16, causal: 508 to 531 us, 1.04 to 1.08 PFLOP/s of the
 // pairs that count.
 #include "ibp_attn.hpp"
 #include "ibp_attn_wave.hpp"
@@ -40,7 +40,9 @@ struct PromptArgs {
 
 constexpr int kWaves = 4;        // of a block, 32 rows each
 constexpr int kBlockRows = 32 * kWaves;
-constexpr float kLazy = 8.f;     // how far (in powers of two) weights may exceed 1
+// How far (in powers of two) weights may exceed those of the reference: 2^8; in float16, with what they are lifted by, 2^15.
+template <class T>
+constexpr float lazy() { return T::kLift ? 15.f - T::kLift : 8.f; }
 
 template <int DIM>
 constexpr int key_tile() { return DIM <= 128 ? 64 : 32; }
@@ -174,8 +176,8 @@ __device__ __forceinline__ void step(const uint8_t *__restrict kt, const uint8_t
             } else {
                 if (f == kTop) {
                     top = max_halves(top);
-                    to = top > r.m + kLazy / c ? fmaxf(r.m, top) : r.m;
-                    mc = to == -inf ? 0.f : to * c;
+                    to = top > r.m + lazy<T>() / c ? fmaxf(r.m, top) : r.m;
+                    mc = base_of<T>(to, c);
                 }
                 constexpr int kShares = kAll - kTop;
                 const int e0 = (f - kTop) * (kElems / 2) / kShares * 2, e1 = (f - kTop + 1) * (kElems / 2) / kShares * 2;
@@ -194,7 +196,7 @@ __device__ __forceinline__ void step(const uint8_t *__restrict kt, const uint8_t
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (S) {
         if (__any(to != r.m)) {          // what there is so far is relative to the old reference
-            const float keep = r.m == -inf ? 0.f : exp2_fast((r.m - to) * c);
+            const float keep = keep_of<T>(r.m, to, c);
             r.l *= keep;
 #pragma unroll
             for (int d = 0; d < DT; ++d) acc[d] *= keep;
@@ -341,7 +343,8 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_prompt
         return;
     }
 
-    l = sum_halves(l);
+    const float unit = unit_of<T>(m, c);
+    l = sum_halves(l) * unit;
     if (row >= q_len) return;
     if (a.splits > 1) {
         const int64_t at = part_at(a, split, head, st.q0 + row);
@@ -353,11 +356,12 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_prompt
             for (int i = 0; i < 4; ++i) {
                 const int to = d * 32 + i * 8 + half * 4;
                 if (to < (int)a.dim)
-                    *reinterpret_cast<f32x4 *>(pp + to) = f32x4{acc[d][i * 4], acc[d][i * 4 + 1], acc[d][i * 4 + 2], acc[d][i * 4 + 3]};
+                    *reinterpret_cast<f32x4 *>(pp + to) =
+                        f32x4{acc[d][i * 4], acc[d][i * 4 + 1], acc[d][i * 4 + 2], acc[d][i * 4 + 3]} * unit;
             }
         return;
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float inv = l == 0.f ? 0.f : unit / l;
     uint8_t *op = (uint8_t *)a.out.data + ((int64_t)(st.q0 + row) * a.out.row + (int64_t)head * a.out.head) * 2;
 #pragma unroll
     for (int d = 0; d < DT; ++d)

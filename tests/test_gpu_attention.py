@@ -115,6 +115,50 @@ def test_prompt_few_rows_many_keys(ibp, kind, heads, kv_heads, dim, causal):
         assert torch.allclose(bad.float(), out.float(), rtol=0.02, atol=0.02)
 
 
+@pytest.mark.parametrize("kind", [F16, BF16])
+@pytest.mark.parametrize("heads,dim,rows,n", [(1, 64, 3, 6000), (1, 128, 2, 300), (600, 64, 2, 9000), (300, 128, 1, 20000), (300, 256, 2, 6000)])
+def test_prompt_one_key_above_many(ibp, kind, heads, dim, rows, n):
+    """One key takes nearly all of the weight and has a value of 0; what the others, at 2^-25 to 2^-30 of its weight,
+    add up to is the output. None of them may be lost, with the keys split (few heads) or not: `attend`'s bound, with
+    float16's spacing taken at the 2^12 by which its weights are lifted before they are rounded."""
+    g = torch.Generator().manual_seed(n)
+    q, k = torch.zeros(rows, 1, dim, dtype=kind), torch.randn(n, 1, dim, generator=g).to(kind)
+    k[:, 0, 0] = -(17.5 + 3.5 * torch.rand(n, generator=g)).to(kind)     # (the rest is not seen by q)
+    q[:, 0, 0] = 1.0
+    v = (0.5 + torch.rand(n, 1, dim, generator=g)).to(kind)
+    k[n // 3, 0, 0], v[n // 3] = 0.0, 0.0
+    out, lse = run_prompt(ibp, q.expand(rows, heads, dim).cuda(), k.cuda(), v.cuda(), [rows], [n], scale=1.0)
+    assert torch.equal(out, out[:, :1].expand_as(out)) and torch.equal(lse, lse[:1].expand_as(lse))
+    o, x, o_tol, x_tol = attend(q[:, 0], k[:, 0], v[:, 0], 1.0, visible(rows, n, True))
+    if kind == F16:
+        o_tol -= 2.0 ** -24 * (1 - 2.0 ** -12) * v[:n - rows + 1, 0].double().sum(0)     # (at least these are seen)
+    assert ((lse[0].double() - x).abs() <= x_tol).all()
+    off = (out[:, 0].double() - o).abs()
+    assert (off <= o_tol).all(), (off / o).max()
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("falling", [False, True])
+@pytest.mark.parametrize("kind", [F16, BF16])
+def test_prompt_scores_of_millions(ibp, kind, falling, causal):
+    """Scores from 0 to 6.5 million in steps of thousands: the largest that a row sees takes all, whatever the
+    reference was before."""
+    n = 1024
+    q, k, v = inputs(kind, 1, 1, 64, [n], [n], seed=37)
+    scores = torch.arange(n, dtype=torch.float32) * 64
+    q[:] = 0
+    q[:, 0, 0] = 1.0
+    k[:, 0, 0] = (scores.flip(0) if falling else scores).to(kind)
+    out, lse = run_prompt(ibp, q, k, v, [n], [n], causal=causal, scale=100.0)
+    for i in range(0, n, 31):
+        seen = k[:i + 1 if causal else n, 0, 0]
+        top = seen.max()
+        best = (seen == top).nonzero()[:, 0]                             # (bfloat16 has several of the largest)
+        want, tol = v[best, 0].double().mean(0), 2.0 ** (-10 if kind == F16 else -7)
+        assert ((out[i, 0].double() - want).abs() <= tol * v[best, 0].double().abs().mean(0) + 2.0 ** -24).all()
+        assert abs(lse[0, i].item() - top.item() * 100.0) <= 2.0 ** -21 * top.item() * 100.0 + len(best)
+
+
 def test_prompt_with_one_workspace_for_all_sizes(ibp):
     """The workspace of the most rows and keys, as one sequence, serves every call of fewer, with the result that a
     workspace of its own gives; what was refused before are the sizes that are split, after one that is not."""
