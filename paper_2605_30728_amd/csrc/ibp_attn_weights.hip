@@ -88,6 +88,17 @@ __device__ __forceinline__ void settle(f32x16 *s, const float *raw, const int *s
     }
 }
 
+// The scores of rows without an lse (raw: -inf) likewise: they may be NaN, which no lse takes away.
+__device__ __forceinline__ void leave_out(f32x16 *s, const float *raw) {
+    const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const bool none = raw[(i >> 2) * 8 + (i & 3) + half * 4] == -__builtin_inff();
+#pragma unroll
+        for (int j = 0; j < 2; ++j) s[j][i] = none ? -__builtin_inff() : s[j][i];
+    }
+}
+
 template <class T, int DIM>
 __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_key_weights(WeightArgs a) {
     constexpr int N = 64, RB = Tile<DIM>::kRowBytes, KS = DIM / 16;
@@ -139,9 +150,9 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_key_we
         for (int i = 0; i < kLoads; ++i) load_to_lds(r, at + i * kWaves * 1024, q_off[i]);
     };
     const float inf = __builtin_inff();
-    auto load_lse = [&](int n) {                             // (rows past the end are like rows without an lse)
+    auto load_lse = [&](int n) {                             // (no row past the end weighs anything)
         const int row = n * N + (int)threadIdx.x;
-        return threadIdx.x < N && row < q_len ? lse[row] : -inf;
+        return threadIdx.x < N && row < q_len ? lse[row] : inf;
     };
     auto put_lse = [&](int buf, float x) {
         if (threadIdx.x >= N) return;
@@ -179,16 +190,18 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_key_we
             load_tile(n + 2, free);
             const int row0 = n * N;
             const uint8_t *qt = lds + here * kTileBytes, *qn = lds + then * kTileBytes;
-            const bool special = row0 < wave_all || row0 + N > q_len || __any(raw != raw);
+            const bool special = row0 < wave_all || row0 + N > q_len || __any(raw != raw), none = __any(raw == -inf);
             if (special) {
                 const int from[2] = {seen[0] - row0, seen[1] - row0};
                 settle(s0, lse_raw[here], from, q_len - row0);
             }
+            if (none) leave_out(s0, lse_raw[here]);
             step<T, DIM>(qt, 32, k, s0, s1, lse_tile[here], sum, a.scale_log2);
             if (special) {
                 const int from[2] = {seen[0] - row0 - 32, seen[1] - row0 - 32};
                 settle(s1, lse_raw[here] + 32, from, q_len - row0 - 32);
             }
+            if (none) leave_out(s1, lse_raw[here] + 32);
             step<T, DIM>(qn, 0, k, s1, s0, lse_tile[here] + 32, sum, a.scale_log2);
             put_lse(free, next_lse);
             tiles_loaded();                                  // (the next tile's second step reads tile n + 2, every wave's share)

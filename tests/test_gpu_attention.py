@@ -384,6 +384,22 @@ def test_key_weights_ignore_what_does_not_count(ibp):
     check_weights(q, k, *lens, lse2, w)
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), NEG])
+@pytest.mark.parametrize("kind,dim", [(BF16, 128), (F16, 64)])
+def test_key_weights_of_rows_without_an_lse(ibp, kind, dim, bad, causal):
+    """A row of lse -inf gives nothing, whatever its query holds, and so whatever its scores are."""
+    lens = [150, 70], [150, 70]
+    q, k, v = inputs(kind, 2, 1, dim, *lens, seed=41)
+    _, lse = run_prompt(ibp, q, k, v, *lens, causal=causal)
+    rows = [0, 33, 64, 149, 150, 219]
+    lse[:, rows] = NEG
+    want = run_weights(ibp, q, k, *lens, lse, causal=causal)
+    check_weights(q, k, *lens, lse, want, causal=causal)
+    q[rows] = bad
+    assert torch.equal(run_weights(ibp, q, k, *lens, lse, causal=causal), want)
+
+
 def test_same_result_every_time_and_on_any_stream(ibp):
     lens = [300, 50], [300, 80]
     q, k, v = inputs(BF16, 8, 2, 128, *lens, seed=23)
