@@ -40,6 +40,9 @@ struct PromptArgs {
 
 constexpr int kWaves = 4;        // of a block, 32 rows each
 constexpr int kBlockRows = 32 * kWaves;
+// The reference is one rounded product, score c, for all exponents: what it is off by they have in common, up to this much times
+// 2^-24, and it cancels in the end; but weights of 2^(this 2^-24) have to be numbers of the type.
+constexpr float kHuge = 0x1p26f;
 // How far (in powers of two) weights may exceed those of the reference: 2^8; in float16, with what they are lifted by, 2^15.
 template <class T>
 constexpr float lazy() { return T::kLift ? 15.f - T::kLift : 8.f; }
@@ -53,7 +56,7 @@ __device__ __forceinline__ int64_t part_at(const PromptArgs &a, int split, int h
 }
 
 // One row, key by key in 32 bits, by one wave: lanes are keys for the scores and columns for the
-// sum. Only for rows whose tiles hold infinities or NaN in places that the row does not see.
+// sum. Only for rows whose tiles hold infinities or NaN in places that the row does not see, and rows of huge scores.
 template <class T, int DIM>
 __device__ void attend_row(const PromptArgs &a, int row, int head, int split, const uint8_t *kp, const uint8_t *vp,
                            int from, int keys) {
@@ -71,7 +74,7 @@ __device__ void attend_row(const PromptArgs &a, int row, int head, int split, co
         float top = s;
         for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
         const float next = fmaxf(m, top), keep = m == -inf ? 0.f : exp2_fast((m - next) * a.scale_log2);
-        const float p = exp2_fast(__builtin_fmaf(s, a.scale_log2, next == -inf ? 0.f : -next * a.scale_log2));
+        const float p = exp2_fast((s - (next == -inf ? 0.f : next)) * a.scale_log2);
         l *= keep;
         for (float &x : acc) x *= keep;
         float sum = p;
@@ -201,6 +204,7 @@ __device__ __forceinline__ void step(const uint8_t *__restrict kt, const uint8_t
 #pragma unroll
             for (int d = 0; d < DT; ++d) acc[d] *= keep;
             r.m = to;
+            r.odd |= fabsf(to * c) >= kHuge && to < inf;
         }
         r.l += sum;
     }

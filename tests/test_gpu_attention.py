@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from attention_reference import attend, key_weights, visible
+from attention_reference import UNIT, attend, key_weights, visible
 
 pytestmark = pytest.mark.gpu
 NEG = float("-inf")
@@ -157,6 +157,41 @@ def test_prompt_scores_of_millions(ibp, kind, falling, causal):
         want, tol = v[best, 0].double().mean(0), 2.0 ** (-10 if kind == F16 else -7)
         assert ((out[i, 0].double() - want).abs() <= tol * v[best, 0].double().abs().mean(0) + 2.0 ** -24).all()
         assert abs(lse[0, i].item() - top.item() * 100.0) <= 2.0 ** -21 * top.item() * 100.0 + len(best)
+
+
+def one_takes_all(q, k, v, scale, seen):
+    """Per row: the value of the key with the highest score and that score, where it is so far above the next that the
+    rest weighs nothing and no rounding of a score matters; None elsewhere."""
+    rows = []
+    for i in range(q.shape[0]):
+        at = seen[i].nonzero()[:, 0]
+        s = k[at].double() @ q[i].double()
+        two = s.topk(min(2, len(at))).values
+        rounding = (k[at].double().abs() @ q[i].double().abs()).max() * q.shape[1] * 2.0 ** -22
+        clear = len(at) == 1 or ((two[0] - two[1]) * scale > 200 and two[0] - two[1] > rounding)
+        rows.append((v[at[s.argmax()]], two[0].item() * scale) if len(at) and clear else None)
+    return rows
+
+
+@pytest.mark.parametrize("scale", [1e7, 1e9, 1e20, 1e30])
+@pytest.mark.parametrize("lens", [([70], [300]), ([1], [1]), ([40, 3], [3100, 2000])], ids=["many", "one", "split"])
+@pytest.mark.parametrize("kind", [BF16, F16])
+def test_prompt_largest_scales(ibp, kind, lens, scale):
+    """Scores of any size that 32 bits hold: one key takes all."""
+    q, k, v = inputs(kind, 2, 1, 64, *lens, seed=43)
+    out, lse = run_prompt(ibp, q, k, v, *lens, scale=scale)
+    q0 = k0 = checked = 0
+    for ql, kl in zip(*lens):
+        for h in range(2):
+            want = one_takes_all(q[q0:q0 + ql, h], k[k0:k0 + kl, 0], v[k0:k0 + kl, 0], scale, visible(ql, kl, True))
+            for i, x in enumerate(want):
+                if x is not None:
+                    off = (out[q0 + i, h].double() - x[0].double()).abs()
+                    assert (off <= 2.02 * UNIT[kind] * x[0].double().abs() + 2.0 ** -24).all()     # its weight's rounding, and its own
+                    assert abs(lse[h, q0 + i].item() - x[1]) <= 2.0 ** -16 * abs(x[1])       # (a score's rounding, 64 products)
+                    checked += 1
+        q0, k0 = q0 + ql, k0 + kl
+    assert checked > sum(lens[0])                                        # of 2 heads
 
 
 def test_prompt_with_one_workspace_for_all_sizes(ibp):
