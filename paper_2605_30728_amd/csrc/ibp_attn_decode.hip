@@ -10,7 +10,7 @@
 // Bound by HBM: every slot's key and value are read once and used by the heads that share them (up to
 // 16 as the columns of one matrix product). They go to registers a chunk ahead of their use, the values on to
 // LDS, which turns them for the second product; the weights are rounded to the inputs' type for it (float16's
-// lifted first, see lift_of), their sum is of the unrounded ones. 131,071 slots of 8 heads of 128 in bf16: 100 us, 5.4 TB/s; 64 sequences of up to
+// lifted first, by kLift), their sum is of the unrounded ones. 131,071 slots of 8 heads of 128 in bf16: 100 us, 5.4 TB/s; 64 sequences of up to
 // 8,192 slots with the slots' weights: 249 us, 4.5 TB/s of what the call has to move (the scores'
 // way through the workspace comes on top). Short caches are bound by two launches: 1,531 slots in 13 us.
 #include "ibp_attn.hpp"
@@ -92,7 +92,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_attn_decode(DecodeArgs a) {
 
     const float inf = __builtin_inff();
     const float c = a.scale_log2;
-    float m = -inf, mc = 0.f, l = 0.f;      // reference, what exponents are relative to, sum
+    float m = -inf, ref = 0.f, l = 0.f;     // reference, what scores are taken relative to (0 while there is none), sum
     f32x4 acc[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = f32x4{};
@@ -170,19 +170,19 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_attn_decode(DecodeArgs a) {
         top = max_halves(max_quarters(top));
         if (__any(top > m)) {
             const float next = fmaxf(m, top);
-            const float keep = keep_of<T>(m, next, c);
+            const float keep = m == -inf ? 0.f : exp2_fast((m - next) * c);
             l *= keep;
 #pragma unroll
             for (int d = 0; d < DT; ++d) acc[d] *= keep;
             m = next;
-            mc = base_of<T>(m, c);
+            ref = m == -inf ? 0.f : m;
         }
         u32x2 p[KT];
 #pragma unroll
         for (int j = 0; j < KT; ++j) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                s[j][i] = exp2_fast(__builtin_fmaf(s[j][i], c, -mc));
+                s[j][i] = exp2_fast(__builtin_fmaf(s[j][i] - ref, c, (float)T::kLift));
                 l += s[j][i];
             }
             p[j][0] = T::pack(s[j][0], s[j][1]);
@@ -202,7 +202,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_attn_decode(DecodeArgs a) {
     }
 
     // the block's waves joined: lane's column is a head, its registers dims quarter * 4 + i
-    const float unit = unit_of<T>(m, c);
+    constexpr float unit = 1.f / (1 << T::kLift);
     l = sum_halves(sum_quarters(l)) * unit;
     if (quarter == 0) {
         stat[wave][0][col] = m;
@@ -345,7 +345,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_attn_decode_join(DecodeArgs a,
 #pragma unroll
             for (int y = 1; y < 64; y <<= 1) sum += __shfl_xor(sum, y);
             if (lane == 0) {
-                part[h * 2] = top == -inf ? 0.f : top * c;
+                part[h * 2] = top == -inf ? 0.f : top;
                 part[h * 2 + 1] = sum == 0.f ? 0.f : 1.f / sum;
             }
         }
@@ -356,7 +356,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_attn_decode_join(DecodeArgs a,
         for (int h = 0; h < heads; ++h) {
             const f32x4 s = *reinterpret_cast<const f32x4 *>(sp + (int64_t)h * a.scores_stride);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] += exp2_fast(__builtin_fmaf(s[i], c, -part[h * 2])) * part[h * 2 + 1];
+            for (int i = 0; i < 4; ++i) w[i] += exp2_fast((s[i] - part[h * 2]) * c) * part[h * 2 + 1];
         }
     }
     float *out = a.weights + ((int64_t)seq * a.kv_heads + kv) * a.weights_stride + slot;

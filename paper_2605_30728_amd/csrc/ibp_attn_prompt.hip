@@ -9,7 +9,7 @@
 // exponential for every pair of a row and a key. Keys and values are read from HBM about once (the heads
 // that share them run on one XCD). A wave holds 32 rows' queries, weights and sums in registers, four waves share
 // the tiles of 64 keys (32 of wide heads) that LDS holds, two of K and two of V. The weights are rounded to the
-// inputs' type for the product with the values, as the matrix unit takes them (float16's lifted first, see lift_of);
+// inputs' type for the product with the values, as the matrix unit takes them (float16's lifted first, by kLift);
 // their sum is of the unrounded ones. 8,192 rows of 32 heads of 128 in bf16, causal: 508 to 531 us, 1.04 to 1.08 PFLOP/s of the
 // pairs that count.
 #include "ibp_attn.hpp"

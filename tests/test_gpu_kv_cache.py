@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from attention_reference import attend, evict
+from attention_reference import UNIT, attend, evict
 
 pytestmark = pytest.mark.gpu
 NEG = float("-inf")
@@ -279,6 +279,33 @@ def test_decode_scores_of_millions(ibp, kind, falling):
     want, tol = v.view(n, 64)[best].double().mean(0), 2.0 ** (-10 if kind == F16 else -7)
     assert ((out[0, 0].cpu().double() - want).abs() <= tol * v.view(n, 64)[best].double().abs().mean(0) + 2.0 ** -24).all()
     assert abs(lse.item() - top.item() * 100.0) <= 2.0 ** -21 * top.item() * 100.0 + len(best)
+
+
+@pytest.mark.parametrize("scale", [1e7, 1e9, 1e20, 1e30])
+@pytest.mark.parametrize("kind,dim", [(BF16, 64), (F16, 64), (F16, 256)])
+def test_decode_largest_scales(ibp, kind, dim, scale):
+    """Scores of any size that 32 bits hold: where one slot is so far above the next that the rest weighs nothing, and no
+    rounding of a score matters, its value is the output (to the rounding of its weight and of the output), and it
+    has a weight of 1 more than before."""
+    c = Cache(kind, 2, dim, [1, 40, 3000, 129], 16, seed=11)
+    q = queries(c, 4, kind)
+    before = torch.zeros(4, 2, 3000)
+    out, lse, after = decode(ibp, c, q, before, scale=scale)
+    checked = 0
+    for b, n in enumerate(c.lens):
+        for h in range(4):
+            k, v = (c.rows(x, b, h // 2, range(n)) for x in (c.k, c.v))
+            s = k.double() @ q[b, h].double()
+            two = s.topk(min(2, n)).values
+            rounding = (k.double().abs() @ q[b, h].double().abs()).max() * dim * 2.0 ** -22
+            if n > 1 and ((two[0] - two[1]) * scale <= 200 or two[0] - two[1] <= rounding):
+                continue
+            want = v[s.argmax()].double()
+            assert ((out[b, h].double() - want).abs() <= 2.02 * UNIT[kind] * want.abs() + 2.0 ** -24).all()
+            assert abs(lse[b, h].item() - two[0].item() * scale) <= 2.0 ** -16 * abs(two[0].item() * scale)
+            before[b, h // 2, s.argmax()] += 1
+            checked += 1
+    assert checked == 16 and (after - before).abs().max() <= 2.0 ** -20
 
 
 def test_decode_with_one_workspace_for_all_sizes(ibp):
