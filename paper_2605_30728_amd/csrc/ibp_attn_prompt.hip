@@ -101,7 +101,7 @@ __device__ void attend_row(const PromptArgs &a, int row, int head, int split, co
     uint16_t *out = (uint16_t *)a.out.data + (int64_t)row * a.out.row + (int64_t)head * a.out.head;
 #pragma unroll
     for (int x = 0; x < (DIM + 63) / 64; ++x)
-        if (lane + 64 * x < (int)a.dim) out[lane + 64 * x] = (uint16_t)T::pack(acc[x] * inv, 0.f);
+        if (lane + 64 * x < (int)a.dim) out[lane + 64 * x] = (uint16_t)T::pack(l == 0.f ? 0.f : acc[x] * inv, 0.f);
     if (a.lse && lane == 0) a.lse[(int64_t)head * a.p.q_rows + row] = l == 0.f ? -inf : m * a.scale + __logf(l);
 }
 
@@ -366,6 +366,10 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_prompt
         return;
     }
     const float inv = l == 0.f ? 0.f : unit / l;
+    if (__any(l == 0.f)) {               // (a weight of 0 may have met an infinity)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) acc[d] = l == 0.f ? f32x16{} : acc[d];
+    }
     uint8_t *op = (uint8_t *)a.out.data + ((int64_t)(st.q0 + row) * a.out.row + (int64_t)head * a.out.head) * 2;
 #pragma unroll
     for (int d = 0; d < DT; ++d)

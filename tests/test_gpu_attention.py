@@ -264,6 +264,22 @@ def test_scores_of_minus_infinity(ibp):
     assert ((out[30:, 0].double() - o).abs() <= o_tol).all() and ((lse[0, 30:].double() - x).abs() <= x_tol).all()
 
 
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("lens", [([70], [70]), ([40], [3100])], ids=["whole", "split"])
+def test_rows_of_no_weight_give_zeros(ibp, lens, bad):
+    """A row that sees only scores of -inf gives zeros, whatever the values are."""
+    (n,), (m,) = lens
+    q, k, v = inputs(F16, 1, 1, 64, *lens, seed=47)
+    q[:, :, 0] = 1.0
+    k[:m - n + 30, :, 0] = NEG
+    at = m - n + 30                          # the keys from here on, which the rows from 30 on see as well
+    _, x, _, x_tol = attend(q[30:, 0], k[at:, 0], v[at:, 0], 64 ** -0.5, visible(n - 30, n - 30, True))
+    v[5, 0, 3], v[m - n + 10] = bad, bad
+    out, lse = run_prompt(ibp, q, k, v, *lens)
+    assert (out[:30] == 0).all() and (lse[0, :30] == NEG).all()
+    assert ((lse[0, 30:].double() - x).abs() <= x_tol).all()
+
+
 def test_prompt_strides(ibp):
     """Heads and rows in any order: slices of one fused tensor, [head][row] order, an output with gaps."""
     lens = [77, 60], [77, 60]
