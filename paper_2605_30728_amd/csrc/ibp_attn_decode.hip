@@ -235,8 +235,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_attn_decode(DecodeArgs a) {
         x *= inv;
         if (last) {
             u32x2 o;
-            o[0] = T::pack(x[0], x[1]);
-            o[1] = T::pack(x[2], x[3]);
+            o[0] = T::pack_out(x[0], x[1]);
+            o[1] = T::pack_out(x[2], x[3]);
             *reinterpret_cast<u32x2 *>((uint8_t *)a.out.data + ((int64_t)seq * a.out.row + (int64_t)head * a.out.head + d) * 2) = o;
         } else {
             *reinterpret_cast<f32x4 *>(a.partial + (((int64_t)seq * a.q_heads + head) * a.splits + split) * a.dim + d) = x;
@@ -319,8 +319,8 @@ __global__ __launch_bounds__(kJoinThreads) void k_attn_decode_join(DecodeArgs a,
         for (int y = 1; y < groups; ++y) o += sums[y * quads + q];
         o *= sum == 0.f ? 0.f : 1.f / sum;
         u32x2 w;
-        w[0] = T::pack(o[0], o[1]);
-        w[1] = T::pack(o[2], o[3]);
+        w[0] = T::pack_out(o[0], o[1]);
+        w[1] = T::pack_out(o[2], o[3]);
         *reinterpret_cast<u32x2 *>((uint8_t *)a.out.data + ((int64_t)seq * a.out.row + (int64_t)head * a.out.head + d) * 2) = w;
         if (a.lse && d == 0) a.lse[(int64_t)seq * a.q_heads + head] = sum == 0.f ? -inf : top * a.scale + __logf(sum);
         return;

@@ -101,7 +101,7 @@ __device__ void attend_row(const PromptArgs &a, int row, int head, int split, co
     uint16_t *out = (uint16_t *)a.out.data + (int64_t)row * a.out.row + (int64_t)head * a.out.head;
 #pragma unroll
     for (int x = 0; x < (DIM + 63) / 64; ++x)
-        if (lane + 64 * x < (int)a.dim) out[lane + 64 * x] = (uint16_t)T::pack(l == 0.f ? 0.f : acc[x] * inv, 0.f);
+        if (lane + 64 * x < (int)a.dim) out[lane + 64 * x] = (uint16_t)T::pack_out(l == 0.f ? 0.f : acc[x] * inv, 0.f);
     if (a.lse && lane == 0) a.lse[(int64_t)head * a.p.q_rows + row] = l == 0.f ? -inf : m * a.scale + __logf(l);
 }
 
@@ -377,8 +377,8 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_prompt
         for (int i = 0; i < 4; ++i) {
             const int at = d * 32 + i * 8 + half * 4;
             u32x2 w;
-            w[0] = T::pack(acc[d][i * 4] * inv, acc[d][i * 4 + 1] * inv);
-            w[1] = T::pack(acc[d][i * 4 + 2] * inv, acc[d][i * 4 + 3] * inv);
+            w[0] = T::pack_out(acc[d][i * 4] * inv, acc[d][i * 4 + 1] * inv);
+            w[1] = T::pack_out(acc[d][i * 4 + 2] * inv, acc[d][i * 4 + 3] * inv);
             if (at < (int)a.dim) *reinterpret_cast<u32x2 *>(op + at * 2) = w;
         }
     if (a.lse && half == 0)
@@ -422,8 +422,8 @@ __global__ __launch_bounds__(256) void k_attn_prompt_join(PromptArgs a) {
         }
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         u32x2 w;
-        w[0] = T::pack(o[0] * inv, o[1] * inv);
-        w[1] = T::pack(o[2] * inv, o[3] * inv);
+        w[0] = T::pack_out(o[0] * inv, o[1] * inv);
+        w[1] = T::pack_out(o[2] * inv, o[3] * inv);
         *reinterpret_cast<u32x2 *>((uint8_t *)a.out.data + ((int64_t)row * a.out.row + (int64_t)head * a.out.head + d) * 2) = w;
         if (a.lse && d == 0) a.lse[(int64_t)head * a.p.q_rows + row] = sum == 0.f ? -inf : top * a.scale + __logf(sum);
     }

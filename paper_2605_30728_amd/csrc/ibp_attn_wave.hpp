@@ -59,6 +59,7 @@ struct Bf16 {
         const f32x2 v = {x, y};
         return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
     }
+    static __device__ __forceinline__ uint32_t pack_out(float x, float y) { return pack(x, y); }
 };
 
 struct F16 {
@@ -80,6 +81,11 @@ struct F16 {
         const f32x2 v = {x, y};
         return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
     }
+    // An output is a mean of values: finite where they are, though its weights' rounding may take it past the largest.
+    static __device__ __forceinline__ float in_range(float x) {
+        return fabsf(x) < __builtin_inff() ? __builtin_amdgcn_fmed3f(x, -65504.f, 65504.f) : x;
+    }
+    static __device__ __forceinline__ uint32_t pack_out(float x, float y) { return pack(in_range(x), in_range(y)); }
 };
 
 // 2^x; a result below the normal range is 0.

@@ -264,6 +264,22 @@ def test_scores_of_minus_infinity(ibp):
     assert ((out[30:, 0].double() - o).abs() <= o_tol).all() and ((lse[0, 30:].double() - x).abs() <= x_tol).all()
 
 
+@pytest.mark.parametrize("heads", [1, 300])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_prompt_of_the_largest_values(ibp, heads, sign):
+    """float16 values of 65504, as a program has that saturates them: so is their mean, whatever the rounding of the
+    weights (of the later keys, each 2^-11 up) makes of it. Infinities stay what they are."""
+    n = 4000
+    q, k, v = (torch.zeros(r, 1, 64, dtype=F16) for r in (2, n, n))
+    q[:, :, 0] = 1.0
+    k[64:, :, 0] = 4.91e-4
+    v[:] = sign * 65504.0
+    v[n // 2, 0, 5] = sign * float("inf")
+    out, lse = run_prompt(ibp, q.expand(2, heads, 64).cuda(), k.cuda(), v.cuda(), [2], [n], scale=1.0)
+    rest = torch.arange(64) != 5
+    assert (out[..., rest].float() == sign * 65504.0).all() and (out[..., 5].float() == sign * float("inf")).all()
+
+
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 @pytest.mark.parametrize("lens", [([70], [70]), ([40], [3100])], ids=["whole", "split"])
 def test_rows_of_no_weight_give_zeros(ibp, lens, bad):

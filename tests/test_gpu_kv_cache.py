@@ -308,6 +308,26 @@ def test_decode_largest_scales(ibp, kind, dim, scale):
     assert checked == 16 and (after - before).abs().max() <= 2.0 ** -20
 
 
+@pytest.mark.parametrize("heads", [1, 512])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_decode_of_the_largest_values(ibp, heads, sign):
+    """float16 values of 65504: so is their mean, whatever the rounding of the weights (all but one 2^-11 up) makes of
+    it. Infinities stay what they are."""
+    n = 4096
+    k, v = (torch.zeros(n // 64, 1, 64, 64, dtype=F16) for _ in range(2))
+    k.view(n, 64)[:, 0] = -1.0                       # with the scale a weight of 0.50025
+    k.view(n, 64)[::32, 0] = 0.0
+    v[:] = sign * 65504.0
+    v.view(n, 64)[n // 2 + 1, 5] = sign * float("inf")
+    q = torch.zeros(1, 1, 64, dtype=F16, device="cuda")
+    q[..., 0] = 1.0
+    out, lse = torch.zeros(1, heads, 64, dtype=F16, device="cuda"), torch.zeros(1, heads, device="cuda")
+    table, lens = torch.arange(n // 64, dtype=torch.int32, device="cuda")[None], torch.tensor([n], dtype=torch.int32, device="cuda")
+    ibp.ibp_attn_decode(q.expand(1, heads, 64), *(x.cuda().expand(-1, heads, -1, -1) for x in (k, v)), table, lens, n, out, lse, scale=0.69265)
+    rest = torch.arange(64) != 5
+    assert (out[..., rest].float() == sign * 65504.0).all() and (out[..., 5].float() == sign * float("inf")).all()
+
+
 def test_decode_with_one_workspace_for_all_sizes(ibp):
     """The workspace of the most sequences and the largest max_len serves every smaller call, on both sides of the
     sizes at which the number of splits falls, with the result that a workspace of its own gives."""
