@@ -137,7 +137,9 @@ def _space(workspace, need, device, stream):
         if stream is None:
             workspace = torch.empty(need, dtype=torch.uint8, device=f"cuda:{device}")
         else:
-            with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
+            if isinstance(stream, int):      # (an ExternalStream of 0 would be one of torch's own)
+                stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream(device)
+            with torch.cuda.stream(stream):
                 workspace = torch.empty(need, dtype=torch.uint8, device=f"cuda:{device}")
     else:
         _array(workspace, "workspace", torch.uint8, device)

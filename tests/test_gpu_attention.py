@@ -523,3 +523,27 @@ def test_workspace_belongs_to_the_stream_of_the_call(ibp, as_handle):
     mine = torch.full((need,), 7, dtype=torch.uint8, device="cuda")
     torch.cuda.synchronize()
     assert (mine == 7).all() and torch.equal(weights, want)
+
+
+@pytest.mark.parametrize("which", ["null", "default", "handle", "current"])
+def test_workspace_is_taken_on_the_stream_of_the_call(ibp, monkeypatch, which):
+    """Whatever names the stream: the default one's handle is 0."""
+    q, k = (torch.randn(n, h, 64, device="cuda").bfloat16() for n, h in ((100, 4), (2000, 2)))
+    at = [torch.tensor([0, n], dtype=torch.int32, device="cuda") for n in (100, 2000)]
+    lse, weights = torch.zeros(4, 100, device="cuda"), torch.zeros(2, 2000, device="cuda")
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    stream, handle = {"null": (0, 0), "default": (torch.cuda.default_stream(), 0), "handle": (other.cuda_stream, other.cuda_stream),
+                      "current": (None, side.cuda_stream)}[which]
+    torch.cuda.synchronize()
+    taken, empty = [], torch.empty
+
+    def recorded(*args, **kwargs):
+        taken.append(torch.cuda.current_stream().cuda_stream)
+        return empty(*args, **kwargs)
+
+    with torch.cuda.stream(side):
+        monkeypatch.setattr(torch, "empty", recorded)
+        ibp.ibp_attn_key_weights(q, k, *at, lse, weights, stream=stream)
+        monkeypatch.undo()
+    torch.cuda.synchronize()
+    assert taken == [handle]
