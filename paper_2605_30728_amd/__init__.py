@@ -393,11 +393,6 @@ def __getattr__(name):
     loaded when first asked for."""
     if name in _ATTENTION or name in ("IBP_BF16", "IBP_F16", "IBP_ATTN_CAUSAL"):
         from . import attention
-        if attention.lib is None:
-            for f, args in attention.SIGS.items():
-                getattr(lib(), f).argtypes = args
-                getattr(lib(), f).restype = ctypes.c_int
-            attention.lib, attention.check = lib, _check
         for n in (*_ATTENTION, "IBP_BF16", "IBP_F16", "IBP_ATTN_CAUSAL"):
             globals()[n] = getattr(attention, n)
         return globals()[name]

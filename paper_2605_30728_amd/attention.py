@@ -11,6 +11,9 @@ import ctypes
 
 import torch
 
+from . import _check as check
+from . import lib
+
 IBP_BF16, IBP_F16 = 0, 1
 IBP_ATTN_CAUSAL = 1
 TYPES = {torch.bfloat16: IBP_BF16, torch.float16: IBP_F16}
@@ -48,8 +51,9 @@ SIGS = {
                      _u64, _vp],
 }
 
-# filled in by the package: the loaded library, the status check
-lib = check = None
+for _f, _args in SIGS.items():
+    getattr(lib(), _f).argtypes = _args
+    getattr(lib(), _f).restype = ctypes.c_int
 
 
 def _tensor(x, what, device):

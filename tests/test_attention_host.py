@@ -1,6 +1,9 @@
 """The attention entry points' checks of arguments (no GPU needed): every call that is refused
 returns before anything is enqueued, with a status and a message."""
 import ctypes
+import os
+import subprocess
+import sys
 
 import pytest
 
@@ -202,3 +205,13 @@ def test_counts_of_more_than_32_bits_are_refused(call, good):
         for bad in (x + (1 << 32), -1):
             with pytest.raises(ValueError):
                 getattr(ibp, call)(*good[:i], bad, *good[i + 1:], *more)
+
+
+@pytest.mark.parametrize("first", ["from paper_2605_30728_amd.attention import ibp_attn_prompt_workspace as f",
+                                   "import paper_2605_30728_amd as ibp; f = ibp.ibp_attn_prompt_workspace",
+                                   "from paper_2605_30728_amd import attention, ibp_attn_prompt_workspace as f; assert f is attention.ibp_attn_prompt_workspace"])
+def test_the_operators_are_reached_from_module_and_package(first):
+    """In a program that has not asked the package for them before."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(ibp.__file__)))
+    done = subprocess.run([sys.executable, "-c", f"{first}; print(f(4, 64, 8, 4096, 1) > 0)"], cwd=root, capture_output=True, text=True)
+    assert (done.returncode, done.stdout.strip()) == (0, "True"), done.stderr
