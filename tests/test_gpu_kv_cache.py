@@ -433,6 +433,23 @@ def test_evict_long(ibp, n, budget, in_place):
     check_evict(c, weights, positions, c.lens, budget, budget // 3, got, in_place)
 
 
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("n", [4095, 4096, 4097, 16383, 16384, 16385, 36863, 36864, 36865])
+def test_evict_at_the_limits_of_what_lds_holds(ibp, n, in_place):
+    """Keys are held in LDS, in arrays of 4,096, 16,384 and 36,864, and above that computed again: the last slot of
+    each and the first beyond it, kept and dropped; one slot too many, and nearly all of them."""
+    c = Cache(BF16, 1, 8, [1, 1], 256, seed=1)       # (its rows are set below)
+    c.lens, c.per = [n, n - 3], -(-n // 256)
+    c.k, c.v = (torch.randn(2 * c.per, 1, 256, 8, generator=torch.Generator().manual_seed(i)).to(BF16) for i in (1, 2))
+    c.table = torch.randperm(2 * c.per, generator=torch.Generator().manual_seed(3)).view(2, c.per).to(torch.int32)
+    for budget, recent, last in ((n - 1, 7, 0.0), (n - 1, 0, 1e9), (100, 3, 1e9)):
+        weights, positions = arrays(c, seed=n)
+        weights[0, 0, -1] = weights[1, 0, n - 4] = last
+        positions[0, 0, -1] = positions[1, 0, n - 4] = -1              # (not kept for its position)
+        got = run_evict(ibp, c, weights, positions, c.lens, budget, recent, in_place)
+        check_evict(c, weights, positions, c.lens, budget, recent, got, in_place)
+
+
 def test_evict_ties_and_special_weights(ibp):
     """Equal weights go by the lowest slot; NaN ranks as -inf, -0 as 0, infinities where they belong."""
     c = Cache(BF16, 3, 64, [300, 300], 16, seed=1)
