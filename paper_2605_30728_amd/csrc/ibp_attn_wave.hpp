@@ -209,10 +209,6 @@ __device__ __forceinline__ void tiles_loaded() {
     asm volatile("" ::: "memory");
 }
 
-__device__ __forceinline__ Frag load_frag(Rsrc r, uint32_t offset) {
-    return __builtin_bit_cast(Frag, __builtin_amdgcn_raw_buffer_load_b128(r, (int)offset, 0, 0));
-}
-
 // Whether any of a fragment's values is infinite or NaN.
 template <class T>
 __device__ __forceinline__ bool has_nonfinite(Frag f) {
