@@ -40,9 +40,11 @@ struct PromptArgs {
 
 constexpr int kWaves = 4;        // of a block, 32 rows each
 constexpr int kBlockRows = 32 * kWaves;
-// The reference is one rounded product, score c, for all exponents: what it is off by they have in common, up to this much times
-// 2^-24, and it cancels in the end; but weights of 2^(this 2^-24) have to be numbers of the type.
-constexpr float kHuge = 0x1p26f;
+// All exponents of a row are taken relative to one rounded product, reference times c. What that is off by, up to 2^-24
+// of it (twice that where weights are lifted), is common to the row's weights and cancels, as long as these are
+// numbers of the type: a row whose reference gets larger than this is done key by key.
+template <class T>
+constexpr float huge() { return T::kLift ? 0x1p23f : 0x1p26f; }
 // How far (in powers of two) weights may exceed those of the reference: 2^8; in float16, with what they are lifted by, 2^15.
 template <class T>
 constexpr float lazy() { return T::kLift ? 15.f - T::kLift : 8.f; }
@@ -180,7 +182,7 @@ __device__ __forceinline__ void step(const uint8_t *__restrict kt, const uint8_t
                 if (f == kTop) {
                     top = max_halves(top);
                     to = top > r.m + lazy<T>() / c ? fmaxf(r.m, top) : r.m;
-                    mc = base_of<T>(to, c);
+                    mc = to == -inf ? 0.f : to * c - (float)T::kLift;
                 }
                 constexpr int kShares = kAll - kTop;
                 const int e0 = (f - kTop) * (kElems / 2) / kShares * 2, e1 = (f - kTop + 1) * (kElems / 2) / kShares * 2;
@@ -199,12 +201,12 @@ __device__ __forceinline__ void step(const uint8_t *__restrict kt, const uint8_t
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (S) {
         if (__any(to != r.m)) {          // what there is so far is relative to the old reference
-            const float keep = keep_of<T>(r.m, to, c);
+            const float keep = r.m == -inf ? 0.f : exp2_fast((r.m - to) * c);
             r.l *= keep;
 #pragma unroll
             for (int d = 0; d < DT; ++d) acc[d] *= keep;
             r.m = to;
-            r.odd |= fabsf(to * c) >= kHuge && to < inf;
+            r.odd |= fabsf(to * c) >= huge<T>() && to < inf;
         }
         r.l += sum;
     }
@@ -347,7 +349,7 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_prompt
         return;
     }
 
-    const float unit = unit_of<T>(m, c);
+    constexpr float unit = 1.f / (1 << T::kLift);
     l = sum_halves(l) * unit;
     if (row >= q_len) return;
     if (a.splits > 1) {

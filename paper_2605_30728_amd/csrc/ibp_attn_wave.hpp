@@ -64,7 +64,11 @@ struct Bf16 {
 
 struct F16 {
     static constexpr uint32_t kExp = 0x7c00u;
-    static constexpr int kLift = 12;             // (see below)
+    // Softmax weights carry this power of two until their row is done. float16 has few exponents: a weight below 2^-14
+    // loses bits and one below 2^-25 counts for nothing in the product with the values, while the sum of the
+    // weights still has it, so that one key far above many others would take what those add up to. Its numbers above 1 are
+    // free: lifted, a weight keeps its bits down to 2^-26 and is there down to 2^-37.
+    static constexpr int kLift = 12;
     static __device__ __forceinline__ float value(uint16_t x) { return (float)__builtin_bit_cast(_Float16, x); }
     static __device__ __forceinline__ f32x16 mfma32(Frag a, Frag b, f32x16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0,
@@ -90,32 +94,6 @@ struct F16 {
 
 // 2^x; a result below the normal range is 0.
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// float16 has few exponents: a softmax weight below 2^-14 loses bits and one below 2^-25 counts for nothing in the
-// product with the values, while the sum of the weights still has it, so that one key far above many others would
-// take what those add up to. Its numbers above 1 are free: a row's weights are lifted by 2^kLift until it
-// is done, which keeps their bits down to 2^-26 and the weights down to 2^-37.
-//
-// Where exponents are taken relative to one rounded product, reference times c (weight = 2^(s c - base)), nothing is
-// lifted by a reference so large that its rounding could carry a weight past the type's largest.
-template <class T>
-__device__ __forceinline__ float lift_of(float reference) {
-    return T::kLift && fabsf(reference) < 0x1p20f ? (float)T::kLift : 0.f;
-}
-template <class T>
-__device__ __forceinline__ float base_of(float m, float c) {
-    return m == -__builtin_inff() ? 0.f : m * c - lift_of<T>(m * c);
-}
-// What weights relative to m are multiplied by when the reference moves to `next`.
-template <class T>
-__device__ __forceinline__ float keep_of(float m, float next, float c) {
-    return m == -__builtin_inff() ? 0.f : exp2_fast((m - next) * c + (lift_of<T>(next * c) - lift_of<T>(m * c)));
-}
-// What takes sums of weights back to ones of exp(s - m), a power of two.
-template <class T>
-__device__ __forceinline__ float unit_of(float m, float c) {
-    return lift_of<T>(m * c) == 0.f ? 1.f : 1.f / (1 << T::kLift);
-}
 
 // x of this lane and of lane ^ 32, combined.
 __device__ __forceinline__ float max_halves(float x) {
