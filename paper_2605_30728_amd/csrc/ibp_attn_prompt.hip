@@ -35,6 +35,7 @@ struct PromptArgs {
     f32x2 *stats;                // splits > 1: [split][q_heads][q rows] reference (in scores) and sum
     float *partial;              //   [split][q_heads][q rows][dim]
     float scale, scale_log2;
+    float lazy, huge;            // lazy<T>() and huge<T>() as scores: over scale_log2
     uint32_t causal;
 };
 
@@ -114,10 +115,18 @@ __device__ __forceinline__ void load_tile(uint8_t *__restrict to, Rsrc r, const 
     for (int i = 0; i < LOADS; ++i) load_to_lds(r, to + i * kWaves * 1024, off[i]);
 }
 
+// What the exponents of a row with reference m are relative to. (Not fused: the lift would take a register all the time,
+// and of those the kernel of 128 wide heads has none left.)
+template <class T>
+__device__ __forceinline__ float base_of(float m, float c) {
+#pragma clang fp contract(off)
+    return m * c - (float)T::kLift;
+}
+
 // A row's running state in its lanes (both halves of the wave agree on m).
 struct Running {
     float m, l;                  // reference (a score) and sum of the weights relative to it
-    bool odd;                    // the row has to be done key by key
+    bool odd;                    // the row has to be done key by key (as one with an infinite reference has)
 };
 
 // The step of tile n for 32 rows of a wave: the weights p of its scores s, the products of the last tile's
@@ -134,7 +143,7 @@ template <class T, int DIM, int N, int LOADS, bool PV, bool S>
 __device__ __forceinline__ void step(const uint8_t *__restrict kt, const uint8_t *__restrict vt, uint8_t *__restrict k_to,
                                      uint8_t *__restrict v_to, Rsrc kr, Rsrc vr, const uint32_t *k_off,
                                      const uint32_t *v_off, const Frag *q, f32x16 *s, f32x16 *next, const Frag *last, Frag *p,
-                                     f32x16 *acc, Running &r, float c) {
+                                     f32x16 *acc, Running &r, float c, float lazy, float huge) {
     constexpr int DT = DIM / 32, NT = N / 32, kPv = PV ? NT * 2 * DT : 0, kS = S ? NT * (DIM / 16) : 0;
     constexpr int kAll = kPv + kS, kElems = S ? NT * 16 : 0;
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
@@ -181,8 +190,8 @@ __device__ __forceinline__ void step(const uint8_t *__restrict kt, const uint8_t
             } else {
                 if (f == kTop) {
                     top = max_halves(top);
-                    to = top > r.m + lazy<T>() / c ? fmaxf(r.m, top) : r.m;
-                    mc = to == -inf ? 0.f : to * c - (float)T::kLift;
+                    to = top > r.m + lazy ? fmaxf(r.m, top) : r.m;
+                    mc = to == -inf ? 0.f : base_of<T>(to, c);
                 }
                 constexpr int kShares = kAll - kTop;
                 const int e0 = (f - kTop) * (kElems / 2) / kShares * 2, e1 = (f - kTop + 1) * (kElems / 2) / kShares * 2;
@@ -205,8 +214,7 @@ __device__ __forceinline__ void step(const uint8_t *__restrict kt, const uint8_t
             r.l *= keep;
 #pragma unroll
             for (int d = 0; d < DT; ++d) acc[d] *= keep;
-            r.m = to;
-            r.odd |= fabsf(to * c) >= huge<T>() && to < inf;
+            r.m = fabsf(to) >= huge ? inf : to;
         }
         r.l += sum;
     }
@@ -311,7 +319,7 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_prompt
         if (pv.value && n * N > wave_all) look(vt);
         step<T, DIM, N, kLoads, pv.value, true>(kt, vt, lk + (n & 1) * kTileBytes, lv + (n & 1) * kTileBytes,
                                                 tile_of(kp, k_stride, n + 2), tile_of(vp, v_stride, n), k_off, v_off, q, s, next,
-                                                last, p, acc, r, c);
+                                                last, p, acc, r, c, a.lazy, a.huge);
     };
     if (some) {
         tiles_loaded();
@@ -336,11 +344,11 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void k_attn_prompt
 #pragma unroll
             for (int i = 0; i < 4; ++i) p0[x][i] = even ? p0[x][i] : p1[x][i];
         step<T, DIM, N, kLoads, true, false>(nullptr, vt, nullptr, nullptr, tile_of(kp, 0, n_tiles), tile_of(vp, 0, n_tiles), k_off,
-                                             v_off, q, s0, s1, p0, p1, acc, r, c);
+                                             v_off, q, s0, s1, p0, p1, acc, r, c, a.lazy, a.huge);
     }
     const float m = r.m;
     float l = r.l;
-    const bool odd = r.odd;
+    const bool odd = r.odd || m == inf;
     if (__any(odd)) {
         const int rows = min(q_len - (tile * kBlockRows + wave * 32), 32);
         for (int r = 0; r < rows; ++r)
@@ -489,7 +497,8 @@ hipError_t launch_prompt(const Shape &s, const Rows &q, const Rows &k, const Row
     if (blocks > kMaxGrid) return hipErrorInvalidConfiguration;
     PromptArgs a{q, k, v, out, p, lse, s.q_heads, s.kv_heads, s.group, s.dim, (uint32_t)tiles, splits,
                  (f32x2 *)workspace, (float *)(workspace + up256((uint64_t)splits * s.q_heads * p.q_rows * 8)), s.scale,
-                 s.scale_log2, s.causal ? 1u : 0u};
+                 s.scale_log2, (s.f16 ? lazy<F16>() : lazy<Bf16>()) / s.scale_log2, (s.f16 ? huge<F16>() : huge<Bf16>()) / s.scale_log2,
+                 s.causal ? 1u : 0u};
     return s.f16 ? prompt_of<F16>(a, (uint32_t)blocks, stream) : prompt_of<Bf16>(a, (uint32_t)blocks, stream);
 }
 
