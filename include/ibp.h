@@ -453,9 +453,10 @@ typedef struct {
  * sees (all of its sequence; with IBP_ATTN_CAUSAL j <= i + keys - queries, places inside the
  * sequence, so that a prompt's last row sees everything before it):
  *   lse_i = ln sum_j exp(x_ij),   out_i = sum_j exp(x_ij - lse_i) v_j.
- * A row that sees no key, or only scores of -inf, gives zeros and an lse of -inf. What a row
- * does not see has no effect on it, infinities and NaN included. d_lse ([q_heads][q rows])
- * may be null. Rows of q outside all sequences leave out and d_lse as they are. Few rows
+ * A row that sees no key, or only scores of -inf, gives zeros and an lse of -inf; one that
+ * sees a score of +inf or NaN gives NaN. What a row does not see has no effect on it,
+ * infinities and NaN included. The weights exp(x_ij - lse_i) are rounded to the inputs' type
+ * for the product with the values, their sum is not. d_lse ([q_heads][q rows]) may be null. Rows of q outside all sequences leave out and d_lse as they are. Few rows
  * against many keys are split along the keys and joined; their parts are in the workspace,
  * which other calls do not use. The workspace of q_rows, k_rows and n_seqs is enough for every
  * call of the same heads with no more rows and no fewer sequences (so n_seqs = 1 serves any
@@ -473,7 +474,8 @@ ibp_status ibp_attn_prompt(const ibp_attn *a, const ibp_rows *q, const ibp_rows 
  *   d_weights[g][j] = sum over the query heads h of KV head g and the rows i that see key j
  *                     of exp(x_ij - d_lse[h][i]),
  * with d_lse as ibp_attn_prompt left it for the same q, k, starts and parameters (a row of
- * lse -inf gives nothing). d_weights is [kv_heads][k rows]; rows of k outside all sequences
+ * lse -inf gives nothing, whatever its q holds). An lse is 32 bits, so that
+ * the weights lose with its size, about 2^-22 |lse| of themselves. d_weights is [kv_heads][k rows]; rows of k outside all sequences
  * leave theirs as they are. The workspace holds the sums of blocks and query heads before
  * they are added up; what n_seqs = 1 needs is enough for any number of sequences.
  */
@@ -510,8 +512,10 @@ ibp_status ibp_attn_decode(const ibp_attn *a, const ibp_rows *q, const ibp_pages
  * in no particular order, which attention does not mind. d_weights and d_positions (distinct
  * within a head) are [sequences][kv_heads][stride], the new ones [sequences][kv_heads]
  * [new_stride] and may be the same arrays (of the same stride); of them the first m slots are
- * written. d_new_lens[s] = m may be d_lens. Pages must not be shared between sequences. Of
- * `a` the type, kv_heads and head_dim are used (a valid q_heads and scale still given).
+ * written. d_new_lens[s] = m may be d_lens; no other output may overlap an input. Pages must
+ * not be shared between sequences, and those of the slots in use must be in the pool: slots
+ * are ranked by weight and position alone, and a move from or to an absent page leaves the
+ * rows as they are. Of `a` the type, kv_heads and head_dim are used (a valid q_heads and scale still given).
  * recent <= budget, budget >= 1, max_len at most 2^31 - 2^24.
  */
 ibp_status ibp_kv_evict_workspace(uint32_t n_seqs, uint32_t kv_heads, uint32_t max_len, uint32_t budget,

@@ -5,7 +5,7 @@ Argument marshalling only, on GPU tensors: torch.bfloat16 or torch.float16 value
 dimension is contiguous and whose other strides are free (multiples of 8); a pool in
 [page][token][head] order is passed as its transposed view. Intermediate results go to `workspace`,
 a uint8 tensor of the size that the _workspace call gives; None takes one from torch's allocator
-for the call.
+for the call. The operators serve inference: results carry no gradient, whatever their inputs ask for.
 """
 import ctypes
 

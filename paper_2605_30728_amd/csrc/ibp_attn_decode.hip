@@ -10,7 +10,7 @@
 // Bound by HBM: every slot's key and value are read once and used by the heads that share them (up to
 // 16 as the columns of one matrix product). They go to registers a chunk ahead of their use, the values on to
 // LDS, which turns them for the second product; the weights are rounded to the inputs' type for it (float16's
-// lifted first, by kLift), their sum is of the unrounded ones. 131,071 slots of 8 heads of 128 in bf16: 100 us, 5.4 TB/s; 64 sequences of up to
+// lifted first, by kLift), their sum is of the unrounded ones. 131,071 slots of 8 heads of 128 in bf16: 101 us, 5.3 TB/s; 64 sequences of up to
 // 8,192 slots with the slots' weights: 249 us, 4.5 TB/s of what the call has to move (the scores'
 // way through the workspace comes on top). Short caches are bound by two launches: 1,531 slots in 13 us.
 #include "ibp_attn.hpp"

@@ -5,13 +5,13 @@
 // in one pass over the keys with a running reference m and a running sum: what has been added up
 // so far is scaled by exp(m_old - m_new) when the reference moves.
 //
-// Bound by the matrix unit and, beside it, by one exponential per pair: 4 DIM operations and one
-// exponential for every pair of a row and a key. Keys and values are read from HBM about once (the heads
+// Every pair of a row and a key costs 4 DIM operations of the matrix unit and, beside it, an exponential. Keys and values are read from HBM about once (the heads
 // that share them run on one XCD). A wave holds 32 rows' queries, weights and sums in registers, four waves share
 // the tiles of 64 keys (32 of wide heads) that LDS holds, two of K and two of V. The weights are rounded to the
 // inputs' type for the product with the values, as the matrix unit takes them (float16's lifted first, by kLift);
-// their sum is of the unrounded ones. 8,192 rows of 32 heads of 128 in bf16, causal: 508 to 531 us, 1.04 to 1.08 PFLOP/s of the
-// pairs that count.
+// their sum is of the unrounded ones. 8,192 rows of 32 heads of 128 in bf16, causal: 512 to 553 us, 0.99 to 1.07 PFLOP/s of
+// the pairs that count, with the matrix unit busy for 0.59 of the time and LDS for 0.30 (of 16 heads of 64, with
+// half the products per exponential, 0.35 and 0.18).
 #include "ibp_attn.hpp"
 #include "ibp_attn_wave.hpp"
 

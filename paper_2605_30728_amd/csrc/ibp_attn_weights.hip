@@ -4,11 +4,15 @@
 // wave as matrix fragments and streams the rows of one query head past them; the query heads of
 // a KV head are added up by a second kernel, so that the result never depends on an order.
 //
-// Bound by the matrix and the vector unit at once: of the pairs of a causal prompt each costs DIM multiply-adds, a
-// subtraction, an exponential and an addition, and nothing of that size is written. 64 keys a wave, since every
-// row fragment read from LDS then feeds two matrix instructions (with 32 keys LDS is as busy as they are);
-// rows reach LDS by direct loads, issued a tile before the one that reads them. 8,192 rows of 32 heads of 128 in bf16: 350 us with the sum
-// over heads, 786 TFLOP/s of the pairs that count.
+// Of the pairs of a causal prompt each costs DIM multiply-adds, a subtraction, an exponential and an addition, and
+// nothing of that size is written. 64 keys a wave, since every row fragment read from LDS then feeds two matrix
+// instructions (with 32 keys LDS is as busy as they are); rows reach LDS by direct loads, issued a tile before the one
+// that reads them. 8,192 rows of 32 heads of 128 in bf16: 351 to 357 us with the sum over heads, 0.77 to 0.78 PFLOP/s
+// of the pairs that count, with the matrix unit busy for 0.40 of the time (11 packed prompts in f16: 82 us, 0.26). What
+// holds both units up shows in the compiled code: the compiler waits for a tile's loads right behind their issue, before
+// the first fragment of the tile at hand is read, which costs every 64 rows a load's latency; and where some pairs of
+// a tile do not count (four tiles or more of every block in a causal prompt) each score reads its row's lse from LDS
+// in a branch of its own (settle).
 #include "ibp_attn.hpp"
 #include "ibp_attn_wave.hpp"
 

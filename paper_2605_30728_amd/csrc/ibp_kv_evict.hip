@@ -305,8 +305,8 @@ hipError_t launch_evict(const Evict &e, uint8_t *workspace, hipStream_t stream) 
     EvictArgs a{e, (int32_t *)workspace, (int32_t *)(workspace + up256(rows * 4)), std::min(e.budget, e.max_len)};
     const uint32_t kept = std::min(e.budget, e.max_len);
     const uint64_t bytes = (uint64_t)std::min(kept, e.max_len - kept) * e.row_bytes * 2;   // moved per head at most
-    // few moves: in the first kernel (a token too many in each of 16 x 8 heads of 2,049 slots: 10.3 us,
-    // with a second launch 12.7), unless the new lengths replace those that its other blocks read
+    // few moves: in the first kernel (a token too many in each of 16 x 8 heads of 2,049 slots: 11.0 us; when this was
+    // chosen 10.3, with a second launch 12.7), unless the new lengths replace those that its other blocks read
     if (std::min(kept, e.max_len - kept) <= kFewMoves && e.new_lens != e.lens) {
         select<true>(a, (uint32_t)rows, stream);
         return hipGetLastError();
