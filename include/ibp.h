@@ -526,6 +526,85 @@ ibp_status ibp_kv_evict(const ibp_attn *a, const ibp_pages *pages, const int32_t
                         int32_t *d_new_positions, uint64_t new_stride, int32_t *d_new_lens, void *workspace,
                         uint64_t workspace_bytes, void *stream);
 
+/*
+ * Writing a paged cache, and holding it in 4 bits. ibp_kv_append brings new rows of keys and values to a
+ * cache's pages, keys turned by their positions, and turns the queries with them; ibp_kv4_append the
+ * same into a cache of records, which ibp_attn_decode4 reads for new tokens, ibp_kv4_read for the next
+ * prompt's attention (as packed rows for ibp_attn_prompt) and ibp_kv_evict evicts from. The conventions are
+ * those of the attention calls. The paper defines none of this.
+ *
+ * A record is what a 4-bit cache holds of one token's key or value of one head, ibp_kv4_record(head_dim)
+ * bytes in groups of 32 values (the last group of a head may be shorter), G of them: 16 G bytes of
+ * codes (byte i of a group has value 2 i in its low half and 2 i + 1 in its high half), G steps, G
+ * centres, both of the cache's type, then padding to 16 bytes that is neither read nor written. A value is
+ *   centre + (code - 7.5) step
+ * of its group. ibp_pages describes pools of records as well: a row is a record, strides count 2 bytes as
+ * ever (multiples of 8). So ibp_kv_evict takes them as rows of record / 2 16-bit values (that as its head_dim), and
+ * a record is a row of a compressed stream like any other.
+ */
+typedef struct {
+    const float *d_table;    /* [positions][turned / 2][2]: cosine and sine, 16-byte aligned */
+    uint64_t positions;
+    uint32_t turned;         /* how many of a head's first values are turned: a multiple of 8; 0: none */
+    uint32_t halves;         /* pairs are value i and i + turned / 2, else 2 i and 2 i + 1 */
+} ibp_rotation;
+
+/*
+ * ibp_kv_append -- rows [d_starts[s], d_starts[s + 1]) of k and v, n of them, become the last n slots of sequence s:
+ * with d_lens[s] slots and the next position d_next[s], both after the call (they may be one array where
+ * nothing was evicted), row i of them goes to slot d_lens[s] - n + i and has position p = d_next[s] - n + i. d_starts
+ * null: every sequence has one row. Each pair (x, y) of a key's turned values becomes
+ *   (x c - y s, x s + y c),  c and s those of p in the rotation's table (p clamped to its positions),
+ * every product and sum rounded to fp32, the results once to the type; values are copied. The same
+ * rows of q, if not null, go turned to q_out, which may be q itself. rotation null: nothing is turned.
+ * If not null, d_weights and d_positions ([sequences][kv_heads][stride], as ibp_kv_evict has them) get 0 and p for the
+ * new slots (those below stride). A row whose slot is negative, beyond the table or of an absent page is not
+ * appended (its query is turned all the same). Rows outside all sequences are left out. Slots
+ * must be distinct: no page may be written for two sequences. Of `a` the type and heads are used (a valid scale still
+ * given). No output may overlap an input otherwise.
+ */
+ibp_status ibp_kv_append(const ibp_attn *a, const ibp_rows *k, const ibp_rows *v, const ibp_rows *q, const ibp_rows *q_out,
+                         const ibp_rotation *rotation, const int32_t *d_starts, uint32_t n_seqs, const ibp_pages *pages,
+                         const int32_t *d_lens, const int32_t *d_next, float *d_weights, int32_t *d_positions,
+                         uint64_t stride, void *stream);
+
+/* ibp_kv4_record -- bytes of a record of head_dim values: 20 per group, rounded up to 16. */
+ibp_status ibp_kv4_record(uint32_t head_dim, uint32_t *bytes);
+
+/*
+ * ibp_kv4_append -- ibp_kv_append into pools of records. Of a group's turned values, in fp32, with lowest lo and highest hi:
+ *   centre = type(lo / 2 + hi / 2),   step = type(max(hi - centre, centre - lo) * (2 / 15)),
+ *   code = (x - centre) * (1 / step) + 7.5, rounded to the nearest (ties to even), clamped to 0 .. 15,
+ * every operation rounded to fp32, type() to the cache's type; 1 / step is 0 for steps below 2^-126. A
+ * group that holds an infinity or NaN, or whose centre or step the type does not hold, stands for NaN (codes 0).
+ */
+ibp_status ibp_kv4_append(const ibp_attn *a, const ibp_rows *k, const ibp_rows *v, const ibp_rows *q, const ibp_rows *q_out,
+                          const ibp_rotation *rotation, const int32_t *d_starts, uint32_t n_seqs, const ibp_pages *pages,
+                          const int32_t *d_lens, const int32_t *d_next, float *d_weights, int32_t *d_positions,
+                          uint64_t stride, void *stream);
+
+/*
+ * ibp_kv4_read -- what slots d_first[s], d_first[s] + 1, ... (d_first null: 0, 1, ...) of a 4-bit cache stand for, into
+ * rows d_starts[s], d_starts[s] + 1, ... of k and v (d_starts null: one row per sequence), values rounded
+ * to fp32 and then to the type. Rows are left as they are from slot d_lens[s] or row d_starts[s + 1] on, where a
+ * slot's page is absent, and outside all sequences: so a history is read to the front of a sequence's rows
+ * whose last ones hold the new turn.
+ */
+ibp_status ibp_kv4_read(const ibp_attn *a, const ibp_pages *pages, const int32_t *d_lens, uint32_t n_seqs,
+                        const int32_t *d_starts, const int32_t *d_first, const ibp_rows *k, const ibp_rows *v,
+                        void *stream);
+
+/*
+ * ibp_attn_decode4 -- ibp_attn_decode over a cache of records: keys and values are what these stand for, exactly.
+ * Queries must be finite (else the head's results are NaN); a group whose step or centre is not finite
+ * gives NaN where it is seen (keys) or in its own columns (values).
+ */
+ibp_status ibp_attn_decode4_workspace(uint32_t n_seqs, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim,
+                                      uint32_t max_len, int weights, uint64_t *bytes);
+ibp_status ibp_attn_decode4(const ibp_attn *a, const ibp_rows *q, const ibp_pages *pages, const int32_t *d_lens,
+                            uint32_t max_len, const ibp_rows *out, float *d_lse, float *d_weights,
+                            uint64_t weights_stride, void *workspace, uint64_t workspace_bytes, void *stream);
+
 /* ibp_last_error -- message of the last failed call on this thread ("" if none).
  * Library plumbing (the paper defines no error reporting). */
 const char *ibp_last_error(void);

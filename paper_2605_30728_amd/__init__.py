@@ -95,7 +95,8 @@ _SIGS = {
 }
 _ATTENTION = ("ibp_attn_prompt_workspace", "ibp_attn_prompt", "ibp_attn_key_weights_workspace", "ibp_attn_key_weights", "ibp_attn_decode_workspace",
               "ibp_attn_decode", "ibp_kv_evict_workspace", "ibp_kv_evict")     # in attention.py, on torch tensors
-EXPORTS = sorted(list(_SIGS) + list(_ATTENTION) + ["ibp_last_error", "ibp_version"])
+_KV_CACHE = ("ibp_kv_append", "ibp_kv4_record", "ibp_kv4_append", "ibp_kv4_read", "ibp_attn_decode4_workspace", "ibp_attn_decode4")   # in kv_cache.py
+EXPORTS = sorted(list(_SIGS) + list(_ATTENTION) + list(_KV_CACHE) + ["ibp_last_error", "ibp_version"])
 
 
 def lib():
@@ -389,11 +390,16 @@ def ibp_cache_destroy(c):
 
 
 def __getattr__(name):
-    """The attention operators need torch's tensors, which the rest of the binding does not: they are
+    """The attention and KV cache operators need torch's tensors, which the rest of the binding does not: they are
     loaded when first asked for."""
     if name in _ATTENTION or name in ("IBP_BF16", "IBP_F16", "IBP_ATTN_CAUSAL"):
         from . import attention
         for n in (*_ATTENTION, "IBP_BF16", "IBP_F16", "IBP_ATTN_CAUSAL"):
             globals()[n] = getattr(attention, n)
+        return globals()[name]
+    if name in _KV_CACHE:
+        from . import kv_cache
+        for n in _KV_CACHE:
+            globals()[n] = getattr(kv_cache, n)
         return globals()[name]
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -19,7 +19,7 @@ ARCH = os.environ.get("IBP_OFFLOAD_ARCH", "gfx950")
 
 HIP_SOURCES = ["ibp_kernels.hip", "ibp_gather_kernels.hip", "ibp_part_kernels.hip", "ibp_cache_kernels.hip", "ibp_runtime.hip",
                "ibp_attn_prompt.hip", "ibp_attn_weights.hip", "ibp_attn_decode.hip", "ibp_kv_evict.hip",
-               "ibp_attn_api.hip"]
+               "ibp_attn_api.hip", "ibp_kv_append.hip", "ibp_attn_decode4.hip", "ibp_kv_api.hip"]
 CXX_SOURCES = ["ibp_host.cpp", "ibp_pool.cpp", "ibp_meta_slots.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", f"-I{INCLUDE}", f"-I{CSRC}"]

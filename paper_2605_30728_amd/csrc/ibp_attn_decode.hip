@@ -13,7 +13,7 @@
 // lifted first, by kLift), their sum is of the unrounded ones. 131,071 slots of 8 heads of 128 in bf16: 101 us, 5.3 TB/s; 64 sequences of up to
 // 8,192 slots with the slots' weights: 249 us, 4.5 TB/s of what the call has to move (the scores'
 // way through the workspace comes on top). Short caches are bound by two launches: 1,531 slots in 13 us.
-#include "ibp_attn.hpp"
+#include "ibp_attn_decode.hpp"
 #include "ibp_attn_wave.hpp"
 
 #include <algorithm>
@@ -25,31 +25,12 @@ namespace {
 
 using namespace dev;
 
-struct DecodeArgs {
-    Rows q, out;
-    Pages pg;
-    const int32_t *lens;
-    float *lse, *weights;
-    uint64_t weights_stride;
-    float *stats;                // [n_seqs][q_heads][splits] pairs: reference (in scores) and sum
-    float *partial;              // [n_seqs][q_heads][splits][dim]
-    float *scores;               // [n_seqs][q_heads][scores_stride], null: not asked for
-    uint32_t scores_stride;
-    uint32_t n_seqs, q_heads, kv_heads, group, head_blocks, dim, max_len;
-    uint32_t split_tokens, splits;
-    float scale, scale_log2;
-};
-
 constexpr int kWaves = 4;
 
 // Slots that a wave takes at a time: what its registers hold of K and V while they are on their
 // way, with two waves per SIMD.
 template <int DIM>
 constexpr int chunk_slots() { return DIM <= 128 ? 32 : 16; }
-
-__device__ __forceinline__ int slots_of(const DecodeArgs &a, uint32_t seq) {
-    return min(max(a.lens[seq], 0), (int)a.max_len);
-}
 
 template <class T, int DIM, bool FULL>
 __global__ __launch_bounds__(64 * kWaves, 2) void k_attn_decode(DecodeArgs a) {
@@ -260,8 +241,6 @@ constexpr int kJoinSlots = 4 * kJoinThreads; // slots whose weights a block of t
 // (512 splits of 256 dims: 16 rounds of its threads instead of 128).
 inline uint32_t join_dims(uint32_t dim, uint32_t splits) { return splits > 64 ? std::min(dim, 64u) : dim; }
 
-constexpr uint32_t kMaxSplits = 1024;
-
 // x over the block's threads, by `op` with neutral element `none`.
 template <class Op>
 __device__ __forceinline__ float block_reduce(float x, float none, float *waves, Op op) {
@@ -415,25 +394,35 @@ uint64_t decode_workspace(uint32_t n_seqs, uint32_t q_heads, uint32_t kv_heads, 
            (weights ? up256(n * q_heads * ((max_len + 31ull) / 32 * 32) * 4) : 0);
 }
 
+namespace {
+uint32_t join_weight_blocks(const DecodeArgs &a) { return a.weights ? (a.max_len + kJoinSlots - 1) / kJoinSlots : 0; }
+}  // namespace
+
+uint64_t decode_join_blocks(const DecodeArgs &a) {
+    const uint32_t dims = join_dims(a.dim, a.splits), dim_blocks = (a.dim + dims - 1) / dims;
+    return (uint64_t)a.n_seqs * a.kv_heads * (join_weight_blocks(a) + (a.splits > 1 ? a.group * dim_blocks : 0));
+}
+
+void launch_decode_join(const DecodeArgs &a, bool f16, hipStream_t stream) {
+    const uint32_t join = (uint32_t)decode_join_blocks(a), dims = join_dims(a.dim, a.splits);
+    if (join == 0) return;
+    if (f16) k_attn_decode_join<F16><<<dim3(join), dim3(kJoinThreads), 0, stream>>>(a, join_weight_blocks(a), dims);
+    else k_attn_decode_join<Bf16><<<dim3(join), dim3(kJoinThreads), 0, stream>>>(a, join_weight_blocks(a), dims);
+}
+
 hipError_t launch_decode(const Shape &s, const Rows &q, const Pages &pg, const int32_t *lens, uint32_t n_seqs,
                          uint32_t max_len, const Rows &out, float *lse, float *weights, uint64_t weights_stride,
                          const DecodePlan &plan, uint8_t *workspace, hipStream_t stream) {
     if (n_seqs == 0) return hipSuccess;
     const uint64_t blocks = (uint64_t)n_seqs * plan.splits * s.kv_heads * plan.head_blocks;
-    const uint32_t weight_blocks = weights ? (max_len + kJoinSlots - 1) / kJoinSlots : 0;
-    const uint32_t dims = join_dims(s.dim, plan.splits), dim_blocks = (s.dim + dims - 1) / dims;
-    const uint64_t join = (uint64_t)n_seqs * s.kv_heads * (weight_blocks + (plan.splits > 1 ? s.group * dim_blocks : 0));
-    if (blocks > kMaxGrid || join > kMaxGrid) return hipErrorInvalidConfiguration;
     DecodeArgs a{q, out, pg, lens, lse, weights, weights_stride, (float *)(workspace + plan.stats_off),
                  (float *)(workspace + plan.out_off), weights ? (float *)(workspace + plan.scores_off) : nullptr,
                  (max_len + 31) / 32 * 32, n_seqs, s.q_heads, s.kv_heads, s.group, plan.head_blocks, s.dim, max_len,
                  plan.split_tokens, plan.splits, s.scale, s.scale_log2};
+    if (blocks > kMaxGrid || decode_join_blocks(a) > kMaxGrid) return hipErrorInvalidConfiguration;
     if (s.f16) decode_of<F16>(a, (uint32_t)blocks, stream);
     else decode_of<Bf16>(a, (uint32_t)blocks, stream);
-    if (join) {
-        if (s.f16) k_attn_decode_join<F16><<<dim3((uint32_t)join), dim3(kJoinThreads), 0, stream>>>(a, weight_blocks, dims);
-        else k_attn_decode_join<Bf16><<<dim3((uint32_t)join), dim3(kJoinThreads), 0, stream>>>(a, weight_blocks, dims);
-    }
+    launch_decode_join(a, s.f16, stream);
     return hipGetLastError();
 }
 

@@ -1,0 +1,207 @@
+"""Binding of the operators that write a paged KV cache and that hold it in 4 bits (include/ibp.h,
+ibp_kv_append, ibp_kv4_* and ibp_attn_decode4).
+
+Argument marshalling only, on GPU tensors as in attention.py. A 4-bit cache's pools are torch.uint8,
+[n_pages][kv_heads][page_tokens][ibp_kv4_record(head_dim)] (strides but the last are free, multiples of
+16); ibp_kv_evict takes them as pool.view(torch.bfloat16).
+"""
+import ctypes
+
+import torch
+
+from . import _check as check
+from . import lib
+from .attention import (TYPES, _array, _attn, _count, _device, _rows, _space, _stream, _tensor, _u32, _u64, _vp, ibp_attn,
+                        ibp_pages, ibp_rows)
+
+
+class ibp_rotation(ctypes.Structure):
+    _fields_ = [("d_table", _vp), ("positions", _u64), ("turned", _u32), ("halves", _u32)]
+
+
+_p = ctypes.POINTER
+_append = [_p(ibp_attn), _p(ibp_rows), _p(ibp_rows), _p(ibp_rows), _p(ibp_rows), _p(ibp_rotation), _vp, _u32, _p(ibp_pages),
+           _vp, _vp, _vp, _vp, _u64, _vp]
+SIGS = {
+    "ibp_kv_append": _append,
+    "ibp_kv4_record": [_u32, _p(_u32)],
+    "ibp_kv4_append": _append,
+    "ibp_kv4_read": [_p(ibp_attn), _p(ibp_pages), _vp, _u32, _vp, _vp, _p(ibp_rows), _p(ibp_rows), _vp],
+    "ibp_attn_decode4_workspace": [_u32, _u32, _u32, _u32, _u32, ctypes.c_int, _p(_u64)],
+    "ibp_attn_decode4": [_p(ibp_attn), _p(ibp_rows), _p(ibp_pages), _vp, _u32, _p(ibp_rows), _vp, _vp, _u64, _vp, _u64, _vp],
+}
+
+for _f, _args in SIGS.items():
+    getattr(lib(), _f).argtypes = _args
+    getattr(lib(), _f).restype = ctypes.c_int
+
+
+def _pool_of(keys, values, table, device, kind, unit, kv_heads, width, what):
+    """Pools [n_pages][kv_heads][page_tokens][width] of one kind; unit: elements of it in 2 bytes."""
+    for x, name in ((keys, "keys"), (values, "values")):
+        _tensor(x, name, device)
+        if x.dtype != kind:
+            raise TypeError(f"{name} must be {kind}, not {x.dtype}")
+        if x.dim() != 4 or x.shape[1] != kv_heads or x.shape[3] != width:
+            raise ValueError(f"{name} must be [n_pages][{kv_heads}][page_tokens][{width}] ({what}), not {list(x.shape)}")
+    if keys.shape != values.shape:
+        raise ValueError("keys and values must have the same shape")
+    table_at = _array(table, "table", torch.int32, device)
+    if table.dim() != 2:
+        raise ValueError("table must be [sequences][pages]")
+    n, h, t, w = keys.shape
+    strides = []
+    for x, name in ((keys, "keys"), (values, "values")):
+        s = x.stride()
+        if s[3] != 1 and w != 1:
+            raise TypeError(f"{name}: the last dimension must be contiguous")
+        for size, stride in zip((n, h, t), s):
+            if size > 1 and stride % (8 * unit):
+                raise ValueError(f"{name}: strides must be multiples of 16 bytes")
+            strides.append(stride // unit if size > 1 else 0)
+    return ibp_pages(keys.data_ptr(), values.data_ptr(), n, t, table.shape[1], table_at, *strides)
+
+
+def _sequences(table, lens, starts, rows, device):
+    """Their number, and the addresses of their lengths and starts."""
+    n = table.shape[0]
+    lens_at = _array(lens, "lens", torch.int32, device, (n,))
+    if starts is None:
+        if rows != n:
+            raise ValueError("without starts every sequence has one row")
+        return n, lens_at, None
+    return n, lens_at, _array(starts, "starts", torch.int32, device, (n + 1,))
+
+
+def _append_to(call, four, k, v, keys, values, table, lens, next_positions, starts, rotation, halves, q, q_out, weights, positions,
+               stream):
+    device = _device(k, "k")
+    kind = k.dtype
+    if kind not in TYPES:
+        raise TypeError(f"k must be bfloat16 or float16, not {kind}")
+    rk = _rows(k, "k", kind, device)
+    rows, kv_heads, dim = k.shape
+    rv = _rows(v, "v", kind, device, kv_heads, dim)
+    if four:
+        pages = _pool_of(keys, values, table, device, torch.uint8, 2, kv_heads, ibp_kv4_record(dim), "records")
+    else:
+        pages = _pool_of(keys, values, table, device, kind, 1, kv_heads, dim, "values")
+    n, lens_at, starts_at = _sequences(table, lens, starts, rows, device)
+    next_at = lens_at if next_positions is lens else _array(next_positions, "next_positions", torch.int32, device, (n,))
+    rq = ro = turn = None
+    heads = kv_heads
+    if q is not None:
+        rq = _rows(q, "q", kind, device)
+        heads = q.shape[1]
+        ro = rq if q_out is None or q_out is q else _rows(q_out, "q_out", kind, device, heads, dim)
+        if q.shape[2] != dim:
+            raise ValueError(f"q must have heads of {dim}, not {q.shape[2]}")
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    if rotation is not None:
+        at = _array(rotation, "rotation", torch.float32, device)
+        if rotation.dim() != 3 or rotation.shape[2] != 2:
+            raise ValueError("rotation must be [positions][pairs][2]")
+        turn = ibp_rotation(at, rotation.shape[0], 2 * rotation.shape[1], bool(halves))
+    slots, weights_at, positions_at = 0, None, None
+    for x, what, t in ((weights, "weights", torch.float32), (positions, "positions", torch.int32)):
+        if x is None:
+            continue
+        at = _array(x, what, t, device)
+        if x.dim() != 3 or x.shape[0] != n or x.shape[1] != kv_heads or slots not in (0, x.shape[2]):
+            raise ValueError("weights and positions must be [sequences][kv_heads][slots]")
+        slots = x.shape[2]
+        if what == "weights":
+            weights_at = at
+        else:
+            positions_at = at
+    a = ibp_attn(TYPES[kind], heads, kv_heads, dim, 1.0, 0)
+    check(getattr(lib(), call)(a, rk, rv, rq, ro, turn, starts_at, n, pages, lens_at, next_at, weights_at, positions_at, slots,
+                               _stream(stream, device)), call)
+
+
+def ibp_kv_append(k, v, keys, values, table, lens, next_positions, starts=None, rotation=None, halves=True, q=None, q_out=None,
+                  weights=None, positions=None, stream=None):
+    """Rows of k and v [rows][kv_heads][dim] become the last slots of their sequences in the pools keys and
+    values [n_pages][kv_heads][page_tokens][dim], keys turned by their positions. starts (int32
+    [sequences + 1]): where each sequence's rows begin; None: one row each. lens and next_positions (int32)
+    are those after the call, and may be one tensor. rotation: float32 [positions][pairs][2], cosine and sine;
+    halves: pairs are (i, i + pairs), else (2 i, 2 i + 1). q [rows][q_heads][dim] is turned into q_out (None: in
+    place). weights (float32) and positions (int32) [sequences][kv_heads][slots] get 0 and the position."""
+    _append_to("ibp_kv_append", False, k, v, keys, values, table, lens, next_positions, starts, rotation, halves, q, q_out, weights,
+               positions, stream)
+
+
+_records = {}
+
+
+def ibp_kv4_record(head_dim):
+    """Bytes of one token's key or value of one head in a 4-bit cache."""
+    got = _records.get(head_dim)
+    if got is None:
+        out = _u32(0)
+        check(lib().ibp_kv4_record(_count(head_dim, "head_dim"), out), "ibp_kv4_record")
+        got = _records[head_dim] = out.value
+    return got
+
+
+def ibp_kv4_append(k, v, keys, values, table, lens, next_positions, starts=None, rotation=None, halves=True, q=None, q_out=None,
+                   weights=None, positions=None, stream=None):
+    """ibp_kv_append into pools of 4-bit records, uint8 [n_pages][kv_heads][page_tokens][ibp_kv4_record(dim)]."""
+    _append_to("ibp_kv4_append", True, k, v, keys, values, table, lens, next_positions, starts, rotation, halves, q, q_out, weights,
+               positions, stream)
+
+
+def ibp_kv4_read(keys, values, table, lens, k, v, starts=None, first=None, stream=None):
+    """What the slots of a 4-bit cache stand for, into packed rows k and v [rows][kv_heads][dim]: slot first[s] + i
+    (first None: i) of sequence s to row starts[s] + i (starts None: one row each), up to lens[s]."""
+    device = _device(k, "k")
+    kind = k.dtype
+    if kind not in TYPES:
+        raise TypeError(f"k must be bfloat16 or float16, not {kind}")
+    rk = _rows(k, "k", kind, device)
+    rows, kv_heads, dim = k.shape
+    rv = _rows(v, "v", kind, device, kv_heads, dim)
+    pages = _pool_of(keys, values, table, device, torch.uint8, 2, kv_heads, ibp_kv4_record(dim), "records")
+    n, lens_at, starts_at = _sequences(table, lens, starts, rows, device)
+    first_at = None if first is None else _array(first, "first", torch.int32, device, (n,))
+    a = ibp_attn(TYPES[kind], kv_heads, kv_heads, dim, 1.0, 0)
+    check(lib().ibp_kv4_read(a, pages, lens_at, n, starts_at, first_at, rk, rv, _stream(stream, device)), "ibp_kv4_read")
+
+
+def ibp_attn_decode4_workspace(n_seqs, q_heads, kv_heads, head_dim, max_len, weights):
+    out = _u64(0)
+    check(lib().ibp_attn_decode4_workspace(_count(n_seqs, "n_seqs"), _count(q_heads, "q_heads"), _count(kv_heads, "kv_heads"),
+                                           _count(head_dim, "head_dim"), _count(max_len, "max_len"), int(bool(weights)), out),
+          "ibp_attn_decode4_workspace")
+    return out.value
+
+
+def ibp_attn_decode4(q, keys, values, table, lens, max_len, out, lse=None, weights=None, scale=None, workspace=None, stream=None):
+    """ibp_attn_decode over a cache of 4-bit records: q and out [sequences][q_heads][dim], the rest as there."""
+    device = _device(q, "q")
+    if q.dtype not in TYPES:
+        raise TypeError(f"q must be bfloat16 or float16, not {q.dtype}")
+    rq = _rows(q, "q", q.dtype, device)
+    n, heads, dim = q.shape
+    _tensor(keys, "keys", device)
+    kv_heads = keys.shape[1] if keys.dim() == 4 else 0
+    pages = _pool_of(keys, values, table, device, torch.uint8, 2, kv_heads, ibp_kv4_record(dim), "records")
+    if table.shape[0] != n:
+        raise ValueError("table must have a row for every sequence")
+    lens_at = _array(lens, "lens", torch.int32, device, (n,))
+    ro = _rows(out, "out", q.dtype, device, heads, dim)
+    lse_at = None if lse is None else _array(lse, "lse", torch.float32, device, (n, heads))
+    weights_at, slots = None, 0
+    if weights is not None:
+        weights_at = _array(weights, "weights", torch.float32, device)
+        if weights.dim() != 3 or weights.shape[:2] != (n, kv_heads):
+            raise ValueError("weights must be [sequences][kv_heads][slots]")
+        slots = weights.shape[2]
+    a = _attn(q, kv_heads, dim, scale)
+    need = 0
+    if workspace is None:
+        need = ibp_attn_decode4_workspace(n, heads, kv_heads, dim, max_len, weights is not None)
+    at, size, held = _space(workspace, need, device, stream)
+    check(lib().ibp_attn_decode4(a, rq, pages, lens_at, _count(max_len, "max_len"), ro, lse_at, weights_at, slots, at, size,
+                                 _stream(stream, device)), "ibp_attn_decode4")
