@@ -1,8 +1,15 @@
 // Attention of one new token per sequence over a paged cache of 4-bit records.
 //
-// The cache's length is split over blocks, which the decode of 16-bit caches' second kernel joins:
-//   x_j = scale sum_d q_d k_jd,   out = sum_j p_j v_j,   k and v = centre + (code - 7.5) step of their group of 32.
+// As in the decode of 16-bit caches the cache's length is split over blocks and a block's waves, and its second kernel
+// joins the blocks. Keys and values are never widened to what they stand for, whose rounding to 16 bits would show: a
+// code is exact as the 16-bit number 16 + code (its bits below those of 16), so that with groups g of 32 values
+//   x_j = scale sum_g [ step_jg sum_d q_d (16 + c_jd)  -  47/2 step_jg sum_d q_d  +  centre_jg sum_d q_d ]
+//   out_d = sum_j (p_j step_jg) (16 + c_jd)  -  47/2 sum_j (p_j step_jg)  +  sum_j p_j centre_jg.
+// A group is what one 16x16x32 product sums over for the keys; the last two terms of a score are one more product of a
+// record's steps and centres with the queries' sums, split into three 16-bit parts (24 bits). The weights times steps are
+// rounded to bfloat16 (two parts of it for a float16 cache, 16 bits), and the same rounded ones meet 16 + c and 47/2.
 #include <algorithm>
+#include <type_traits>
 
 #include "ibp_attn_decode.hpp"
 #include "ibp_attn_wave.hpp"
@@ -15,106 +22,405 @@ namespace {
 
 using namespace dev;
 
-// Four values of a record from place d on.
+constexpr int kWaves = 4;
+constexpr int kChunk = 64;               // slots that a wave takes at a time: a lane looks up each one's page
+
+// The layout of a chunk's records in LDS: rows of an odd number of 16-byte pieces, so that the 16 keys of
+// a product are in different banks.
+template <int G>
+struct Rec {
+    static constexpr int kBytes = record_bytes(G * kGroupValues), kPieces = kBytes / 16;
+    static constexpr int kRow = kPieces % 2 ? kBytes : kBytes + 16;
+    static constexpr int kMeta = G * kGroupBytes, kMetaFrags = (G + 3) / 4, kStepDwords = (G + 1) / 2;
+    static constexpr int kSide = kChunk * kRow;
+};
+
+// Eight codes as 16-bit numbers 16 + code, values i and i + 4 of them side by side.
 template <class T>
-__device__ __forceinline__ f32x4 values_at(const uint8_t *record, uint32_t d, uint32_t groups) {
-    const uint32_t code = *reinterpret_cast<const uint16_t *>(record + d / 2);
-    const uint8_t *meta = record + groups * kGroupBytes + d / kGroupValues * 2;
-    const float step = T::value(*reinterpret_cast<const uint16_t *>(meta)), centre = T::value(*reinterpret_cast<const uint16_t *>(meta + groups * 2));
-    f32x4 x;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = __builtin_fmaf((float)(code >> 4 * i & 15) - 7.5f, step, centre);
-    return x;
+__device__ __forceinline__ Frag widen_codes(uint32_t x);
+template <>
+__device__ __forceinline__ Frag widen_codes<Bf16>(uint32_t x) {
+    constexpr uint32_t m = 0x00780078u, k = 0x41804180u;
+    return Frag{(x << 3 & m) | k, (x >> 1 & m) | k, (x >> 5 & m) | k, (x >> 9 & m) | k};
+}
+template <>
+__device__ __forceinline__ Frag widen_codes<F16>(uint32_t x) {
+    constexpr uint32_t m = 0x03c003c0u, k = 0x4c004c00u;
+    return Frag{(x << 6 & m) | k, (x << 2 & m) | k, (x >> 2 & m) | k, (x >> 6 & m) | k};
 }
 
-// A wave per split and query head, slot by slot; a lane has four values of the head.
+// The two 16-bit halves of a dword as numbers.
 template <class T>
-__global__ __launch_bounds__(64) void k_attn_decode4(DecodeArgs a) {
-    const uint32_t head = blockIdx.x % a.q_heads, seq = blockIdx.x / a.q_heads % a.n_seqs, split = blockIdx.x / a.q_heads / a.n_seqs;
-    const uint32_t kv = head / a.group, groups = record_groups(a.dim), d = threadIdx.x * 4;
-    const int len = slots_of(a, seq), from = split * a.split_tokens, to = from < len ? from + min(len - from, (int)a.split_tokens) : from;
-    if (from >= to && split) return;
-    const bool in = d < a.dim;
-    const float inf = __builtin_inff(), c = a.scale_log2;
-    float q[4] = {};
-    if (in)
-        for (int i = 0; i < 4; ++i)
-            q[i] = T::value(*(reinterpret_cast<const uint16_t *>(a.q.data) + (int64_t)seq * a.q.row + (int64_t)head * a.q.head + d + i));
-    float m = -inf, l = 0.f;
-    f32x4 acc{};
-    float *sp = a.scores ? a.scores + ((int64_t)seq * a.q_heads + head) * a.scores_stride : nullptr;
-    for (int slot = from; slot < to; ++slot) {
-        const uint32_t i = a.pg.page_magic ? __umulhi(slot, a.pg.page_magic) >> a.pg.page_shift : (uint32_t)slot >> a.pg.page_shift;
-        const int32_t page = a.pg.table[(int64_t)seq * a.pg.table_stride + i];
-        const bool there = (uint32_t)page < a.pg.n_pages;
-        float x = -inf;
-        f32x4 v{};
-        if (there) {
-            const int64_t row = slot - i * a.pg.page_tokens;
-            const uint8_t *kr = (const uint8_t *)a.pg.k.data + ((int64_t)page * a.pg.k.page + (int64_t)kv * a.pg.k.head + row * a.pg.k.token) * 2;
-            const uint8_t *vr = (const uint8_t *)a.pg.v.data + ((int64_t)page * a.pg.v.page + (int64_t)kv * a.pg.v.head + row * a.pg.v.token) * 2;
-            float sum = 0.f;
-            if (in) {
-                const f32x4 k = values_at<T>(kr, d, groups);
-                v = values_at<T>(vr, d, groups);
-                for (int y = 0; y < 4; ++y) sum = __builtin_fmaf(q[y], k[y], sum);
+__device__ __forceinline__ float low(uint32_t x) {
+    return T::value((uint16_t)x);
+}
+template <class T>
+__device__ __forceinline__ float high(uint32_t x) {
+    if constexpr (std::is_same_v<T, Bf16>) return __uint_as_float(x & 0xffff0000u);
+    else return T::value((uint16_t)(x >> 16));
+}
+
+// 16 rows of 16 codes, transposed over 16 lanes: lane i gets code i of the rows whose addresses the lanes pass.
+__device__ __forceinline__ u32x2 read_codes(const uint8_t *p) {
+    typedef int v2i __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr4_b64_v2i32((IBP_LDS(v2i) *)p));
+}
+// Four rows of 16 16-bit numbers, the same.
+__device__ __forceinline__ u32x2 read_numbers(const uint8_t *p) {
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((IBP_LDS(s16x4) *)p));
+}
+
+// Key `row` of the t-th product of a chunk is this slot of it: those that a quarter of the wave has
+// of all four products are spread over the banks.
+__device__ __forceinline__ int slot_of(int t, int row) { return t * 16 + (row ^ (t & 1) * 8); }
+
+template <class T, int G>
+__global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void k_attn_decode4(DecodeArgs a) {
+    using R = Rec<G>;
+    constexpr int DIM = G * kGroupValues, DT = DIM / 16, NP = R::kPieces, MF = R::kMetaFrags;
+    constexpr int kParts = std::is_same_v<T, F16> ? 2 : 1;
+    constexpr int kJoin = 16 * (DIM + 4) * 4;        // a wave's sums, for the join
+    constexpr int kWaveBytes = (2 * R::kSide + 16 > kJoin ? 2 * R::kSide + 16 : kJoin) + 15 & ~15;
+    __shared__ __align__(128) uint8_t lds[kWaves * kWaveBytes];
+    __shared__ float stat[kWaves][2][16];
+    __shared__ __align__(16) float sums[kWaves][16][16];
+
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), quarter = lane >> 4, col = lane & 15;
+    const uint32_t hb = blockIdx.x % (a.kv_heads * a.head_blocks), rest = blockIdx.x / (a.kv_heads * a.head_blocks);
+    // (splits outermost: those that no sequence reaches come last; and sequences turned by one from split
+    // to split, so that each one's splits run on all XCDs)
+    const uint32_t split = rest / a.n_seqs, seq = (rest % a.n_seqs + split) % a.n_seqs;
+    const uint32_t kv = hb / a.head_blocks, head0 = kv * a.group + hb % a.head_blocks * 16;
+    const int heads = min((int)((kv + 1) * a.group - head0), 16);
+    const int len = uniform(slots_of(a, seq));
+    const int from = split * a.split_tokens, to = from < len ? from + min(len - from, (int)a.split_tokens) : from;
+    if (from >= to && !(split == 0)) return;
+
+    // the queries, in the order of widen_codes, and the products' second operand for steps and centres
+    Frag q[G], qs[MF];
+    float back = 1.f;                    // what its product is to be multiplied with
+    {
+        const uint8_t *qp = (const uint8_t *)a.q.data + ((int64_t)seq * a.q.row + (int64_t)(head0 + min(col, heads - 1)) * a.q.head) * 2;
+        float side[MF * 8];              // -47/2 sum and sum of every group, in the order of a record's steps and centres
+#pragma unroll
+        for (int i = 0; i < MF * 8; ++i) side[i] = 0.f;
+        float top = 0.f;
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            const Frag f = load_head<false>(qp, g * kGroupValues + quarter * 8, a.dim);
+            float x = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x += low<T>(f[i]) + high<T>(f[i]);
+            x = sum_halves(sum_quarters(x));
+            side[g] = -23.5f * x;
+            side[G + g] = x;
+            top = fmaxf(top, fabsf(side[g]));
+            q[g] = Frag{(f[0] & 0xffffu) | f[2] << 16, f[0] >> 16 | (f[2] & 0xffff0000u), (f[1] & 0xffffu) | f[3] << 16,
+                        f[1] >> 16 | (f[3] & 0xffff0000u)};
+        }
+        if constexpr (kParts == 2) {     // float16: the largest brought to 2^14, so that no part is lost below or above
+            const int e = top > 0.f && top < __builtin_inff() ? (int)(__float_as_uint(top) >> 23) - 127 - 14 : 0;
+            back = __builtin_amdgcn_ldexpf(1.f, e);
+#pragma unroll
+            for (int i = 0; i < MF * 8; ++i) side[i] = __builtin_amdgcn_ldexpf(side[i], -e);
+        }
+        // quarter 0, 1 and 2 have the first, second and third part
+#pragma unroll
+        for (int i = 0; i < MF * 8; i += 2) {
+            float x = side[i], y = side[i + 1];
+            uint32_t part = T::pack(x, y);
+#pragma unroll
+            for (int n = 1; n < 3; ++n) {
+                x -= low<T>(part);
+                y -= high<T>(part);
+                const uint32_t next = T::pack(x, y);
+                part = quarter >= n ? next : part;
             }
-            for (int y = 1; y < 64; y <<= 1) sum += __shfl_xor(sum, y);
-            x = sum;
+            qs[i / 8][i % 8 / 2] = quarter == 3 ? 0u : part;
         }
-        if (sp && threadIdx.x == 0) sp[slot] = x;
-        if (x > m) {
-            const float keep = m == -inf ? 0.f : exp2_fast((m - x) * c);
+    }
+
+    // lane i knows the page of slot i of a chunk, and its place there
+    const int32_t *table = a.pg.table + (int64_t)seq * a.pg.table_stride;
+    int page = 0, place = 0;
+    auto find = [&](int chunk) {
+        const uint32_t s = min(chunk + lane, len - 1);
+        const uint32_t i = a.pg.page_magic ? __umulhi(s, a.pg.page_magic) >> a.pg.page_shift : s >> a.pg.page_shift;
+        place = (int)(s - i * a.pg.page_tokens);
+        page = table[i];
+    };
+
+    const float inf = __builtin_inff();
+    const float c = a.scale_log2;
+    float m = -inf, ref = 0.f, l = 0.f;     // reference, what scores are taken relative to (0 while there is none), sum
+    f32x4 acc[DT], z{};                     // out, and the weighted sums of steps and centres
+#pragma unroll
+    for (int d = 0; d < DT; ++d) acc[d] = f32x4{};
+    uint8_t *ks = lds + wave * kWaveBytes, *vs = ks + R::kSide;
+
+    constexpr int kStep = kWaves * kChunk;
+    Frag kf[NP], vf[NP];
+    uint64_t live = 0;                   // bit i: slot i of the chunk is there
+    const uint8_t *kbase = (const uint8_t *)a.pg.k.data + (int64_t)kv * a.pg.k.head * 2;
+    const uint8_t *vbase = (const uint8_t *)a.pg.v.data + (int64_t)kv * a.pg.v.head * 2;
+    // the loads of a chunk whose pages are known, and the look-up of the next one's, so that
+    // nothing waits for a look-up
+    auto load = [&](int chunk) {
+        const bool in = (uint32_t)page < a.pg.n_pages;
+        live = __ballot(in && chunk + lane < len);
+        const int pg = in ? page : 0;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int x = i * 64 + lane, slot = x / NP, piece = x % NP;
+            const int64_t p = __shfl(pg, slot), r = __shfl(place, slot);
+            kf[i] = *reinterpret_cast<const Frag *>(kbase + (p * a.pg.k.page + r * a.pg.k.token) * 2 + piece * 16);
+            vf[i] = *reinterpret_cast<const Frag *>(vbase + (p * a.pg.v.page + r * a.pg.v.token) * 2 + piece * 16);
+        }
+        find(chunk + kStep);
+    };
+
+    int chunk = from + wave * kChunk;
+    if (chunk < to) {
+        find(chunk);
+        load(chunk);
+    }
+    for (; chunk < to; chunk += kStep) {
+        const uint64_t now = live;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int x = i * 64 + lane, slot = x / NP, piece = x % NP;
+            if (now != ~0ull) {          // slots that are not there: zeros
+                const uint32_t keep = now >> slot & 1 ? ~0u : 0u;
+                kf[i] &= keep;
+                vf[i] &= keep;
+            }
+            if constexpr (G % 4 != 0) {  // a record's padding, which may hold anything: zeros
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const bool used = piece * 16 + w * 4 < R::kMeta + G * 4;
+                    kf[i][w] = used ? kf[i][w] : 0u;
+                    vf[i][w] = used ? vf[i][w] : 0u;
+                }
+            }
+            *reinterpret_cast<Frag *>(ks + slot * R::kRow + piece * 16) = kf[i];
+            *reinterpret_cast<Frag *>(vs + slot * R::kRow + piece * 16) = vf[i];
+        }
+        if (chunk + kStep < to) load(chunk + kStep);
+
+        f32x4 s[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const uint8_t *key = ks + slot_of(t, col) * R::kRow;
+            f32x4 side{};
+#pragma unroll
+            for (int f = 0; f < MF; ++f) side = T::mfma16(*reinterpret_cast<const Frag *>(key + R::kMeta + f * 16), qs[f], side);
+            const uint8_t *steps = ks + slot_of(t, quarter * 4) * R::kRow + R::kMeta;
+            uint32_t st[4][R::kStepDwords];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int w = 0; w < R::kStepDwords; ++w) st[i][w] = *reinterpret_cast<const uint32_t *>(steps + i * R::kRow + w * 4);
+            s[t] = side * back;
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const Frag code = widen_codes<T>(*reinterpret_cast<const uint32_t *>(key + g * kGroupBytes + quarter * 4));
+                const f32x4 x = T::mfma16(code, q[g], f32x4{});
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    s[t][i] = __builtin_fmaf(g % 2 ? high<T>(st[i][g / 2]) : low<T>(st[i][g / 2]), x[i], s[t][i]);
+            }
+        }
+        if (now != ~0ull) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (!(now >> (slot_of(t, quarter * 4) + i) & 1)) s[t][i] = -inf;
+        }
+        if (a.scores && col < heads) {
+            float *sp = a.scores + ((int64_t)seq * a.q_heads + head0 + col) * a.scores_stride + chunk;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4 *>(sp + slot_of(t, quarter * 4)) = s[t];
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][i]);
+        top = max_halves(max_quarters(top));
+        if (__any(top > m)) {
+            const float next = fmaxf(m, top);
+            const float keep = m == -inf ? 0.f : exp2_fast((m - next) * c);
             l *= keep;
-            acc *= keep;
-            m = x;
+            z *= keep;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) acc[d] *= keep;
+            m = next;
+            ref = m == -inf ? 0.f : m;
         }
-        if (!there) continue;
-        const float p = exp2_fast((x - (m == -inf ? 0.f : m)) * c);
-        l += p;
-        acc += p * v;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[t][i] = exp2_fast(__builtin_fmaf(s[t][i] - ref, c, (float)T::kLift));
+                l += s[t][i];
+            }
+            const uint8_t *meta = vs + slot_of(t, quarter * 4 + (col >> 2)) * R::kRow + R::kMeta + (col & 3) * 8;
+            z = T::mfma16(read_numbers(meta), u32x2{T::pack(s[t][0], s[t][1]), T::pack(s[t][2], s[t][3])}, z);
+        }
+        const uint8_t *codes = vs + slot_of(col >> 2, quarter * 4 + (col & 3)) * R::kRow;
+        const Frag minus = Frag{0xc1bcc1bcu, 0xc1bcc1bcu, 0xc1bcc1bcu, 0xc1bcc1bcu};     // -47/2
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            Frag p[kParts][2];
+#pragma unroll
+            for (int t = 0; t < 4; t += 2)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float x[2];
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const uint32_t st = *reinterpret_cast<const uint32_t *>(vs + (slot_of(t + y, quarter * 4) + i) * R::kRow + R::kMeta + g / 2 * 4);
+                        x[y] = s[t + y][i] * (g % 2 ? high<T>(st) : low<T>(st));
+                    }
+                    p[0][t / 2][i] = Bf16::pack(x[0], x[1]);
+                    if constexpr (kParts == 2)
+                        p[1][t / 2][i] = Bf16::pack(x[0] - low<Bf16>(p[0][t / 2][i]), x[1] - high<Bf16>(p[0][t / 2][i]));
+                }
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const u32x2 x = read_codes(codes + g * kGroupBytes + half * 8);
+                f32x4 o = acc[g * 2 + half];
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const Frag code = widen_codes<Bf16>(x[y]);
+#pragma unroll
+                    for (int n = 0; n < kParts; ++n) {
+                        o = Bf16::mfma16(minus, p[n][y], o);
+                        o = Bf16::mfma16(code, p[n][y], o);
+                    }
+                }
+                acc[g * 2 + half] = o;
+            }
+        }
     }
+
+    // the block's waves joined: lane's column is a head, its registers dims quarter * 4 + i (of z: a record's numbers)
+    constexpr float unit = 1.f / (1 << T::kLift);
+    l = sum_halves(sum_quarters(l)) * unit;
+    if (quarter == 0) {
+        stat[wave][0][col] = m;
+        stat[wave][1][col] = l;
+    }
+    *reinterpret_cast<f32x4 *>(&sums[wave][col][quarter * 4]) = z;
+    __syncthreads();
+    float *mine = reinterpret_cast<float *>(ks);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+        *reinterpret_cast<f32x4 *>(mine + col * (DIM + 4) + d * 16 + quarter * 4) = (acc[d] + sums[wave][col][G + d / 2]) * unit;
+    __syncthreads();
+    const int h = threadIdx.x >> 4;          // 16 heads, 16 threads each
+    if (h >= heads) return;
+    float top = -inf, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, stat[w][0][h]);
+    float part[kWaves];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        part[w] = part_of(stat[w][0][h], stat[w][1][h], top, c);
+        if (!(part[w] < 0.f)) sum += part[w] * stat[w][1][h];
+    }
+    const uint32_t head = head0 + h;
     const bool last = a.splits == 1;
-    const int64_t part = ((int64_t)seq * a.q_heads + head) * a.splits + split;
-    if (threadIdx.x == 0) {
-        if (last && a.lse) a.lse[(int64_t)seq * a.q_heads + head] = l == 0.f ? -inf : m * a.scale + __logf(l);
-        if (!last || a.weights) {
-            a.stats[part * 2] = m;
-            a.stats[part * 2 + 1] = l;
+    const float inv = !last ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+    for (int d = (threadIdx.x & 15) * 4; d < (int)a.dim; d += 64) {
+        f32x4 x{};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w)
+            if (!(part[w] < 0.f)) x += part[w] * *reinterpret_cast<const f32x4 *>(reinterpret_cast<float *>(lds + w * kWaveBytes) + h * (DIM + 4) + d);
+        x *= inv;
+        if (last) {
+            u32x2 o;
+            o[0] = T::pack_out(x[0], x[1]);
+            o[1] = T::pack_out(x[2], x[3]);
+            *reinterpret_cast<u32x2 *>((uint8_t *)a.out.data + ((int64_t)seq * a.out.row + (int64_t)head * a.out.head + d) * 2) = o;
+        } else {
+            *reinterpret_cast<f32x4 *>(a.partial + (((int64_t)seq * a.q_heads + head) * a.splits + split) * a.dim + d) = x;
         }
     }
-    if (!in) return;
-    if (last) {
-        acc *= l == 0.f ? 0.f : 1.f / l;
-        *reinterpret_cast<u32x2 *>((uint8_t *)a.out.data + ((int64_t)seq * a.out.row + (int64_t)head * a.out.head + d) * 2) =
-            u32x2{T::pack_out(acc[0], acc[1]), T::pack_out(acc[2], acc[3])};
-    } else {
-        *reinterpret_cast<f32x4 *>(a.partial + part * a.dim + d) = acc;
+    if ((threadIdx.x & 15) == 0) {
+        if (last && a.lse) a.lse[(int64_t)seq * a.q_heads + head] = sum == 0.f ? -inf : top * a.scale + __logf(sum);
+        if (!last || a.weights) {
+            float *st = a.stats + (((int64_t)seq * a.q_heads + head) * a.splits + split) * 2;
+            st[0] = top;
+            st[1] = sum;
+        }
     }
 }
+
+template <class T>
+void decode4_of(const DecodeArgs &a, uint32_t blocks, hipStream_t stream) {
+    const dim3 grid(blocks), block(64 * kWaves);
+    switch (record_groups(a.dim)) {
+    case 1: k_attn_decode4<T, 1><<<grid, block, 0, stream>>>(a); break;
+    case 2: k_attn_decode4<T, 2><<<grid, block, 0, stream>>>(a); break;
+    case 3: k_attn_decode4<T, 3><<<grid, block, 0, stream>>>(a); break;
+    case 4: k_attn_decode4<T, 4><<<grid, block, 0, stream>>>(a); break;
+    case 5: k_attn_decode4<T, 5><<<grid, block, 0, stream>>>(a); break;
+    case 6: k_attn_decode4<T, 6><<<grid, block, 0, stream>>>(a); break;
+    case 7: k_attn_decode4<T, 7><<<grid, block, 0, stream>>>(a); break;
+    default: k_attn_decode4<T, 8><<<grid, block, 0, stream>>>(a); break;
+    }
+}
+
+uint64_t up256(uint64_t x) { return (x + 255) / 256 * 256; }
+uint32_t scores_stride(uint32_t max_len) { return (max_len + 63) / 64 * 64; }
+
+constexpr uint32_t kMinSplit = kWaves * kChunk;      // a chunk for every wave
+constexpr uint32_t kManySplit = 1536;
 
 }  // namespace
 
 DecodePlan plan_decode4(uint32_t n_seqs, uint32_t q_heads, uint32_t kv_heads, uint32_t dim, uint32_t max_len, bool weights) {
-    return plan_decode(n_seqs, q_heads, kv_heads, dim, max_len, weights);
+    DecodePlan p{};
+    p.head_blocks = (q_heads / kv_heads + 15) / 16;
+    const uint64_t rows = std::max<uint64_t>((uint64_t)n_seqs * kv_heads * p.head_blocks, 1), len = std::max<uint64_t>(max_len, 1);
+    uint64_t t = n_seqs > 1 ? std::min<uint64_t>((len * rows + 1023) / 1024, kManySplit) : (len * rows + 511) / 512;
+    t = std::max<uint64_t>(t, (len + kMaxSplits - 1) / kMaxSplits);
+    t = (std::min(t, len) + kMinSplit - 1) / kMinSplit * kMinSplit;
+    p.split_tokens = (uint32_t)t;
+    p.splits = (uint32_t)((len + t - 1) / t);
+    const uint64_t parts = (uint64_t)n_seqs * q_heads * p.splits;
+    p.stats_off = 0;
+    p.out_off = up256(parts * 8);
+    p.scores_off = p.out_off + (p.splits > 1 ? up256(parts * dim * 4) : 0);
+    p.bytes = p.scores_off + (weights ? up256((uint64_t)n_seqs * q_heads * scores_stride(max_len) * 4) : 0);
+    return p;
 }
 
+// What plan_decode4 needs at most for up to n_seqs sequences of up to max_len slots: by its rule a sequence has a split for
+// every kMinSplit slots at most, and no more than both kManySplit slots each and 1,024 blocks among all sequences
+// (each rounded up) come to; this grows with both sizes.
 uint64_t decode4_workspace(uint32_t n_seqs, uint32_t q_heads, uint32_t kv_heads, uint32_t dim, uint32_t max_len, bool weights) {
-    return decode_workspace(n_seqs, q_heads, kv_heads, dim, max_len, weights);
+    const uint64_t n = n_seqs, len = std::max<uint64_t>(max_len, 1), blocks = (uint64_t)kv_heads * ((q_heads / kv_heads + 15) / 16);
+    const uint64_t splits = std::min(n * std::min<uint64_t>((len + kMinSplit - 1) / kMinSplit, kMaxSplits),
+                                     std::max((1024 + blocks - 1) / blocks + n, n * ((len + kManySplit - 1) / kManySplit)));
+    return up256(splits * q_heads * 8) + (len > kMinSplit ? up256(splits * q_heads * dim * 4) : 0) +
+           (weights ? up256(n * q_heads * scores_stride(max_len) * 4) : 0);
 }
 
 hipError_t launch_decode4(const Shape &s, const Rows &q, const Pages &pg, const int32_t *lens, uint32_t n_seqs,
                           uint32_t max_len, const Rows &out, float *lse, float *weights, uint64_t weights_stride,
                           const DecodePlan &plan, uint8_t *workspace, hipStream_t stream) {
     if (n_seqs == 0) return hipSuccess;
-    const uint64_t blocks = (uint64_t)n_seqs * plan.splits * s.q_heads;
+    const uint64_t blocks = (uint64_t)n_seqs * plan.splits * s.kv_heads * plan.head_blocks;
     DecodeArgs a{q, out, pg, lens, lse, weights, weights_stride, (float *)(workspace + plan.stats_off),
                  (float *)(workspace + plan.out_off), weights ? (float *)(workspace + plan.scores_off) : nullptr,
-                 (max_len + 31) / 32 * 32, n_seqs, s.q_heads, s.kv_heads, s.group, plan.head_blocks, s.dim, max_len,
+                 scores_stride(max_len), n_seqs, s.q_heads, s.kv_heads, s.group, plan.head_blocks, s.dim, max_len,
                  plan.split_tokens, plan.splits, s.scale, s.scale_log2};
     if (blocks > kMaxGrid || decode_join_blocks(a) > kMaxGrid) return hipErrorInvalidConfiguration;
-    if (s.f16) k_attn_decode4<F16><<<dim3((uint32_t)blocks), dim3(64), 0, stream>>>(a);
-    else k_attn_decode4<Bf16><<<dim3((uint32_t)blocks), dim3(64), 0, stream>>>(a);
+    if (s.f16) decode4_of<F16>(a, (uint32_t)blocks, stream);
+    else decode4_of<Bf16>(a, (uint32_t)blocks, stream);
     launch_decode_join(a, s.f16, stream);
     return hipGetLastError();
 }
