@@ -25,29 +25,31 @@ using namespace dev;
 constexpr int kWaves = 4;
 constexpr int kChunk = 64;               // slots that a wave takes at a time: a lane looks up each one's page
 
-// The layout of a chunk's records in LDS: rows of an odd number of 16-byte pieces, so that the 16 keys of
-// a product are in different banks.
+// A chunk's keys, then its values, in LDS: rows of codes of an odd number of 16-byte pieces, so that the 16 keys of a product are in
+// different banks; the records' steps and centres as they are; and the steps in 32 bits, [group][slot].
 template <int G>
 struct Rec {
-    static constexpr int kBytes = record_bytes(G * kGroupValues), kPieces = kBytes / 16;
-    static constexpr int kRow = kPieces % 2 ? kBytes : kBytes + 16;
-    static constexpr int kMeta = G * kGroupBytes, kMetaFrags = (G + 3) / 4, kStepDwords = (G + 1) / 2;
-    static constexpr int kSide = kChunk * kRow;
+    static constexpr int kMetaFrags = (G + 3) / 4, kCodes = G * kGroupBytes;
+    static constexpr int kRow = (G | 1) * 16, kMetaRow = kMetaFrags * 16;
+    static constexpr int kMeta = kChunk * kRow, kSteps = kMeta + kChunk * kMetaRow + 16, kBytes = kSteps + G * kChunk * 4;
 };
 
-// Eight codes as 16-bit numbers 16 + code, values i and i + 4 of them side by side.
+// What turns codes into 16-bit numbers: where they lie in these, and 16. Kept out of the compiler's sight, in a scalar and a
+// vector register, so that masking and setting are one instruction (constants it would take apart).
 template <class T>
-__device__ __forceinline__ Frag widen_codes(uint32_t x);
-template <>
-__device__ __forceinline__ Frag widen_codes<Bf16>(uint32_t x) {
-    constexpr uint32_t m = 0x00780078u, k = 0x41804180u;
-    return Frag{(x << 3 & m) | k, (x >> 1 & m) | k, (x >> 5 & m) | k, (x >> 9 & m) | k};
-}
-template <>
-__device__ __forceinline__ Frag widen_codes<F16>(uint32_t x) {
-    constexpr uint32_t m = 0x03c003c0u, k = 0x4c004c00u;
-    return Frag{(x << 6 & m) | k, (x << 2 & m) | k, (x >> 2 & m) | k, (x >> 6 & m) | k};
-}
+struct Widen {
+    uint32_t mask, sixteen;
+    __device__ __forceinline__ Widen() {
+        asm("s_mov_b32 %0, %1" : "=s"(mask) : "n"(std::is_same_v<T, Bf16> ? 0x00780078 : 0x03c003c0));
+        asm("v_mov_b32 %0, %1" : "=v"(sixteen) : "n"(std::is_same_v<T, Bf16> ? 0x41804180 : 0x4c004c00));
+    }
+    // Eight codes, values i and i + 4 of them side by side.
+    __device__ __forceinline__ Frag operator()(uint32_t x) const {
+        constexpr bool b = std::is_same_v<T, Bf16>;
+        return Frag{((b ? x << 3 : x << 6) & mask) | sixteen, ((b ? x >> 1 : x << 2) & mask) | sixteen,
+                    ((b ? x >> 5 : x >> 2) & mask) | sixteen, ((b ? x >> 9 : x >> 6) & mask) | sixteen};
+    }
+};
 
 // The two 16-bit halves of a dword as numbers.
 template <class T>
@@ -75,12 +77,12 @@ __device__ __forceinline__ u32x2 read_numbers(const uint8_t *p) {
 __device__ __forceinline__ int slot_of(int t, int row) { return t * 16 + (row ^ (t & 1) * 8); }
 
 template <class T, int G>
-__global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void k_attn_decode4(DecodeArgs a) {
+__global__ __launch_bounds__(64 * kWaves, G <= 4 ? 3 : 2) void k_attn_decode4(DecodeArgs a) {
     using R = Rec<G>;
-    constexpr int DIM = G * kGroupValues, DT = DIM / 16, NP = R::kPieces, MF = R::kMetaFrags;
+    constexpr int DIM = G * kGroupValues, DT = DIM / 16, MF = R::kMetaFrags;
     constexpr int kParts = std::is_same_v<T, F16> ? 2 : 1;
     constexpr int kJoin = 16 * (DIM + 4) * 4;        // a wave's sums, for the join
-    constexpr int kWaveBytes = (2 * R::kSide + 16 > kJoin ? 2 * R::kSide + 16 : kJoin) + 15 & ~15;
+    constexpr int kWaveBytes = R::kBytes > kJoin ? R::kBytes : kJoin;
     __shared__ __align__(128) uint8_t lds[kWaves * kWaveBytes];
     __shared__ float stat[kWaves][2][16];
     __shared__ __align__(16) float sums[kWaves][16][16];
@@ -96,18 +98,42 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void k_attn_decode4(De
     const int from = split * a.split_tokens, to = from < len ? from + min(len - from, (int)a.split_tokens) : from;
     if (from >= to && !(split == 0)) return;
 
-    // the queries, in the order of widen_codes, and the products' second operand for steps and centres
+    Frag raw[G];                         // the queries, used once the first records are on their way
+    {
+        const uint8_t *qp = (const uint8_t *)a.q.data + ((int64_t)seq * a.q.row + (int64_t)(head0 + min(col, heads - 1)) * a.q.head) * 2;
+#pragma unroll
+        for (int g = 0; g < G; ++g) raw[g] = load_head<false>(qp, g * kGroupValues + quarter * 8, a.dim);
+    }
+
+    // lane i looks up the page of slot i of a chunk
+    const int32_t *table = a.pg.table + (int64_t)seq * a.pg.table_stride;
+    int page = 0, place = 0;
+    auto find = [&](int chunk) {
+        const uint32_t s = min(chunk + lane, len - 1);
+        const uint32_t i = a.pg.page_magic ? __umulhi(s, a.pg.page_magic) >> a.pg.page_shift : s >> a.pg.page_shift;
+        place = (int)(s - i * a.pg.page_tokens);
+        page = table[i];
+    };
+
+    const Widen<T> widen_k;
+    const Widen<Bf16> widen_v;
+    const float inf = __builtin_inff();
+    const float c = a.scale_log2;
+    float m = -inf, ref = 0.f, l = 0.f;     // reference, what scores are taken relative to (0 while there is none), sum
+    f32x4 acc[DT], z{};                     // out, and the weighted sums of steps and centres
+#pragma unroll
+    for (int d = 0; d < DT; ++d) acc[d] = f32x4{};
+    // the queries, in the order of Widen, and the products' second operand for steps and centres
     Frag q[G], qs[MF];
     float back = 1.f;                    // what its product is to be multiplied with
     {
-        const uint8_t *qp = (const uint8_t *)a.q.data + ((int64_t)seq * a.q.row + (int64_t)(head0 + min(col, heads - 1)) * a.q.head) * 2;
         float side[MF * 8];              // -47/2 sum and sum of every group, in the order of a record's steps and centres
 #pragma unroll
         for (int i = 0; i < MF * 8; ++i) side[i] = 0.f;
         float top = 0.f;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            const Frag f = load_head<false>(qp, g * kGroupValues + quarter * 8, a.dim);
+            const Frag f = raw[g];
             float x = 0.f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) x += low<T>(f[i]) + high<T>(f[i]);
@@ -140,102 +166,95 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void k_attn_decode4(De
         }
     }
 
-    // lane i knows the page of slot i of a chunk, and its place there
-    const int32_t *table = a.pg.table + (int64_t)seq * a.pg.table_stride;
-    int page = 0, place = 0;
-    auto find = [&](int chunk) {
-        const uint32_t s = min(chunk + lane, len - 1);
-        const uint32_t i = a.pg.page_magic ? __umulhi(s, a.pg.page_magic) >> a.pg.page_shift : s >> a.pg.page_shift;
-        place = (int)(s - i * a.pg.page_tokens);
-        page = table[i];
-    };
+    uint8_t *tile = lds + wave * kWaveBytes, *meta = tile + R::kMeta;
+    float *steps = reinterpret_cast<float *>(tile + R::kSteps);
 
-    const float inf = __builtin_inff();
-    const float c = a.scale_log2;
-    float m = -inf, ref = 0.f, l = 0.f;     // reference, what scores are taken relative to (0 while there is none), sum
-    f32x4 acc[DT], z{};                     // out, and the weighted sums of steps and centres
-#pragma unroll
-    for (int d = 0; d < DT; ++d) acc[d] = f32x4{};
-    uint8_t *ks = lds + wave * kWaveBytes, *vs = ks + R::kSide;
-
+    // Keys and values take turns in the same registers and the same LDS: values are on their way during the products with the keys, the
+    // next chunk's keys during those with the values. A lane loads pieces of codes, neighbours neighbouring ones, and
+    // the steps and centres of its own slot.
     constexpr int kStep = kWaves * kChunk;
-    Frag kf[NP], vf[NP];
+    Frag codes[G], numbers[MF];
+    int64_t value_at = 0;                // of this lane's slot
     uint64_t live = 0;                   // bit i: slot i of the chunk is there
     const uint8_t *kbase = (const uint8_t *)a.pg.k.data + (int64_t)kv * a.pg.k.head * 2;
     const uint8_t *vbase = (const uint8_t *)a.pg.v.data + (int64_t)kv * a.pg.v.head * 2;
-    // the loads of a chunk whose pages are known, and the look-up of the next one's, so that
-    // nothing waits for a look-up
-    auto load = [&](int chunk) {
+    auto of_slot = [](int64_t x, int slot) {         // lane `slot`'s x
+        return (int64_t)((uint64_t)(uint32_t)__shfl((int)(x >> 32), slot) << 32 | (uint32_t)__shfl((int)x, slot));
+    };
+    auto load = [&](const uint8_t *base, int64_t at) {
+#pragma unroll
+        for (int i = 0; i < MF; ++i) numbers[i] = *reinterpret_cast<const Frag *>(base + at + R::kCodes + i * 16);
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            const int x = i * 64 + lane;
+            codes[i] = *reinterpret_cast<const Frag *>(base + of_slot(at, x / G) + x % G * 16);
+        }
+    };
+    auto load_keys = [&](int chunk) {
         const bool in = (uint32_t)page < a.pg.n_pages;
         live = __ballot(in && chunk + lane < len);
-        const int pg = in ? page : 0;
+        const int64_t pg = in ? page : 0;
+        value_at = (pg * a.pg.v.page + (int64_t)place * a.pg.v.token) * 2;
+        load(kbase, (pg * a.pg.k.page + (int64_t)place * a.pg.k.token) * 2);
+    };
+    auto store = [&](uint64_t live) {
+        const bool there = live >> lane & 1;         // else steps and centres of 0: it counts for nothing
 #pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            const int x = i * 64 + lane, slot = x / NP, piece = x % NP;
-            const int64_t p = __shfl(pg, slot), r = __shfl(place, slot);
-            kf[i] = *reinterpret_cast<const Frag *>(kbase + (p * a.pg.k.page + r * a.pg.k.token) * 2 + piece * 16);
-            vf[i] = *reinterpret_cast<const Frag *>(vbase + (p * a.pg.v.page + r * a.pg.v.token) * 2 + piece * 16);
+        for (int i = 0; i < MF; ++i) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w)              // (what follows a record's numbers may be anything)
+                numbers[i][w] = i * 4 + w < G && there ? numbers[i][w] : 0u;
+            *reinterpret_cast<Frag *>(meta + lane * R::kMetaRow + i * 16) = numbers[i];
         }
-        find(chunk + kStep);
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            const uint32_t x = numbers[g / 8][g % 8 / 2];
+            steps[g * kChunk + lane] = g % 2 ? high<T>(x) : low<T>(x);
+        }
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            const int x = i * 64 + lane;
+            *reinterpret_cast<Frag *>(tile + x / G * R::kRow + x % G * 16) = codes[i];
+        }
     };
 
     int chunk = from + wave * kChunk;
     if (chunk < to) {
         find(chunk);
-        load(chunk);
+        load_keys(chunk);
     }
     for (; chunk < to; chunk += kStep) {
         const uint64_t now = live;
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            const int x = i * 64 + lane, slot = x / NP, piece = x % NP;
-            if (now != ~0ull) {          // slots that are not there: zeros
-                const uint32_t keep = now >> slot & 1 ? ~0u : 0u;
-                kf[i] &= keep;
-                vf[i] &= keep;
-            }
-            if constexpr (G % 4 != 0) {  // a record's padding, which may hold anything: zeros
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const bool used = piece * 16 + w * 4 < R::kMeta + G * 4;
-                    kf[i][w] = used ? kf[i][w] : 0u;
-                    vf[i][w] = used ? vf[i][w] : 0u;
-                }
-            }
-            *reinterpret_cast<Frag *>(ks + slot * R::kRow + piece * 16) = kf[i];
-            *reinterpret_cast<Frag *>(vs + slot * R::kRow + piece * 16) = vf[i];
-        }
-        if (chunk + kStep < to) load(chunk + kStep);
+        store(now);
+        load(vbase, value_at);
+        find(chunk + kStep);
 
         f32x4 s[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            const uint8_t *key = ks + slot_of(t, col) * R::kRow;
+            const int row = slot_of(t, col), mine = slot_of(t, quarter * 4);
             f32x4 side{};
 #pragma unroll
-            for (int f = 0; f < MF; ++f) side = T::mfma16(*reinterpret_cast<const Frag *>(key + R::kMeta + f * 16), qs[f], side);
-            const uint8_t *steps = ks + slot_of(t, quarter * 4) * R::kRow + R::kMeta;
-            uint32_t st[4][R::kStepDwords];
+            for (int f = 0; f < MF; ++f) side = T::mfma16(*reinterpret_cast<const Frag *>(meta + row * R::kMetaRow + f * 16), qs[f], side);
+            f32x4 x[G];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int w = 0; w < R::kStepDwords; ++w) st[i][w] = *reinterpret_cast<const uint32_t *>(steps + i * R::kRow + w * 4);
+            for (int g = 0; g < G; ++g)
+                x[g] = T::mfma16(widen_k(*reinterpret_cast<const uint32_t *>(tile + row * R::kRow + g * kGroupBytes + quarter * 4)), q[g], f32x4{});
             s[t] = side * back;
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                const Frag code = widen_codes<T>(*reinterpret_cast<const uint32_t *>(key + g * kGroupBytes + quarter * 4));
-                const f32x4 x = T::mfma16(code, q[g], f32x4{});
+                const f32x4 step = *reinterpret_cast<const f32x4 *>(steps + g * kChunk + mine);
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    s[t][i] = __builtin_fmaf(g % 2 ? high<T>(st[i][g / 2]) : low<T>(st[i][g / 2]), x[i], s[t][i]);
+                for (int i = 0; i < 4; ++i) s[t][i] = __builtin_fmaf(step[i], x[g][i], s[t][i]);
             }
         }
         if (now != ~0ull) {
+            const uint64_t there[2] = {now >> (quarter * 4), now >> (quarter * 4 ^ 8)};      // of even and of odd products
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (!(now >> (slot_of(t, quarter * 4) + i) & 1)) s[t][i] = -inf;
+                    if (!(there[t & 1] >> (t * 16 + i) & 1)) s[t][i] = -inf;
         }
         if (a.scores && col < heads) {
             float *sp = a.scores + ((int64_t)seq * a.q_heads + head0 + col) * a.scores_stride + chunk;
@@ -265,35 +284,37 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void k_attn_decode4(De
                 s[t][i] = exp2_fast(__builtin_fmaf(s[t][i] - ref, c, (float)T::kLift));
                 l += s[t][i];
             }
-            const uint8_t *meta = vs + slot_of(t, quarter * 4 + (col >> 2)) * R::kRow + R::kMeta + (col & 3) * 8;
-            z = T::mfma16(read_numbers(meta), u32x2{T::pack(s[t][0], s[t][1]), T::pack(s[t][2], s[t][3])}, z);
         }
-        const uint8_t *codes = vs + slot_of(col >> 2, quarter * 4 + (col & 3)) * R::kRow;
+
+        store(now);
+        if (chunk + kStep < to) load_keys(chunk + kStep);
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+            z = T::mfma16(read_numbers(meta + slot_of(t, quarter * 4 + (col >> 2)) * R::kMetaRow + (col & 3) * 8),
+                          u32x2{T::pack(s[t][0], s[t][1]), T::pack(s[t][2], s[t][3])}, z);
+        const uint8_t *transposed = tile + slot_of(col >> 2, quarter * 4 + (col & 3)) * R::kRow;
         const Frag minus = Frag{0xc1bcc1bcu, 0xc1bcc1bcu, 0xc1bcc1bcu, 0xc1bcc1bcu};     // -47/2
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             Frag p[kParts][2];
 #pragma unroll
-            for (int t = 0; t < 4; t += 2)
+            for (int y = 0; y < 2; ++y) {
+                const f32x4 u = s[y * 2] * *reinterpret_cast<const f32x4 *>(steps + g * kChunk + slot_of(y * 2, quarter * 4));
+                const f32x4 v = s[y * 2 + 1] * *reinterpret_cast<const f32x4 *>(steps + g * kChunk + slot_of(y * 2 + 1, quarter * 4));
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    float x[2];
-#pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        const uint32_t st = *reinterpret_cast<const uint32_t *>(vs + (slot_of(t + y, quarter * 4) + i) * R::kRow + R::kMeta + g / 2 * 4);
-                        x[y] = s[t + y][i] * (g % 2 ? high<T>(st) : low<T>(st));
-                    }
-                    p[0][t / 2][i] = Bf16::pack(x[0], x[1]);
+                    p[0][y][i] = Bf16::pack(u[i], v[i]);
                     if constexpr (kParts == 2)
-                        p[1][t / 2][i] = Bf16::pack(x[0] - low<Bf16>(p[0][t / 2][i]), x[1] - high<Bf16>(p[0][t / 2][i]));
+                        p[1][y][i] = Bf16::pack(u[i] - low<Bf16>(p[0][y][i]), v[i] - high<Bf16>(p[0][y][i]));
                 }
+            }
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                const u32x2 x = read_codes(codes + g * kGroupBytes + half * 8);
+                const u32x2 x = read_codes(transposed + g * kGroupBytes + half * 8);
                 f32x4 o = acc[g * 2 + half];
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    const Frag code = widen_codes<Bf16>(x[y]);
+                    const Frag code = widen_v(x[y]);
 #pragma unroll
                     for (int n = 0; n < kParts; ++n) {
                         o = Bf16::mfma16(minus, p[n][y], o);
@@ -314,7 +335,7 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 2 : 1) void k_attn_decode4(De
     }
     *reinterpret_cast<f32x4 *>(&sums[wave][col][quarter * 4]) = z;
     __syncthreads();
-    float *mine = reinterpret_cast<float *>(ks);
+    float *mine = reinterpret_cast<float *>(tile);
 #pragma unroll
     for (int d = 0; d < DT; ++d)
         *reinterpret_cast<f32x4 *>(mine + col * (DIM + 4) + d * 16 + quarter * 4) = (acc[d] + sums[wave][col][G + d / 2]) * unit;
