@@ -6,8 +6,14 @@
 //   x_j = scale sum_g [ step_jg sum_d q_d (16 + c_jd)  -  47/2 step_jg sum_d q_d  +  centre_jg sum_d q_d ]
 //   out_d = sum_j (p_j step_jg) (16 + c_jd)  -  47/2 sum_j (p_j step_jg)  +  sum_j p_j centre_jg.
 // A group is what one 16x16x32 product sums over for the keys; the last two terms of a score are one more product of a
-// record's steps and centres with the queries' sums, split into three 16-bit parts (24 bits). The weights times steps are
-// rounded to bfloat16 (two parts of it for a float16 cache, 16 bits), and the same rounded ones meet 16 + c and 47/2.
+// record's steps and centres with the queries' sums, split into three 16-bit parts (24 bits).
+//
+// The weights times steps p_j step_jg are rounded for the product with the codes, and the same rounded ones meet 16 + c and 47/2. In
+// bfloat16 that would show as much as the rounding of the output does (error against 64 bits 0.0023 of the output instead of
+// 0.0017), so a bfloat16 cache's are float16 numbers (39 us for the long cache below instead of 37.5), its steps scaled so that
+// the largest so far is from 4 to 8 and weights lifted by 2^12 as float16 weights are elsewhere: they have 11 bits
+// down to 2^-28 of the largest step and are there down to 2^-39. A float16 cache's are two bfloat16 parts, 16 bits at any
+// size (for a bfloat16 cache that took 45 us).
 #include <algorithm>
 #include <type_traits>
 
@@ -72,6 +78,18 @@ __device__ __forceinline__ u32x2 read_numbers(const uint8_t *p) {
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((IBP_LDS(s16x4) *)p));
 }
 
+// The largest of x over a wave.
+__device__ __forceinline__ float max_wave(float x) {
+    auto turned = [](float v, auto by) {             // of the 16 lanes that a lane is one of
+        return __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0x120 + decltype(by)::value, 0xf, 0xf, true));
+    };
+    x = fmaxf(x, turned(x, std::integral_constant<int, 8>{}));
+    x = fmaxf(x, turned(x, std::integral_constant<int, 4>{}));
+    x = fmaxf(x, turned(x, std::integral_constant<int, 2>{}));
+    x = fmaxf(x, turned(x, std::integral_constant<int, 1>{}));
+    return __uint_as_float((uint32_t)uniform((int)__float_as_uint(max_halves(max_quarters(x)))));
+}
+
 // Key `row` of the t-th product of a chunk is this slot of it: those that a quarter of the wave has
 // of all four products are spread over the banks.
 __device__ __forceinline__ int slot_of(int t, int row) { return t * 16 + (row ^ (t & 1) * 8); }
@@ -80,7 +98,10 @@ template <class T, int G>
 __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 3 : 2) void k_attn_decode4(DecodeArgs a) {
     using R = Rec<G>;
     constexpr int DIM = G * kGroupValues, DT = DIM / 16, MF = R::kMetaFrags;
-    constexpr int kParts = std::is_same_v<T, F16> ? 2 : 1;
+    constexpr bool kHalf = std::is_same_v<T, F16>;
+    using P = std::conditional_t<kHalf, Bf16, F16>;  // of the weights times steps, kParts numbers each
+    constexpr int kParts = kHalf ? 2 : 1;
+    constexpr int kLift = F16::kLift;                // of the weights, until the slots are done
     constexpr int kJoin = 16 * (DIM + 4) * 4;        // a wave's sums, for the join
     constexpr int kWaveBytes = R::kBytes > kJoin ? R::kBytes : kJoin;
     __shared__ __align__(128) uint8_t lds[kWaves * kWaveBytes];
@@ -115,8 +136,8 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 3 : 2) void k_attn_decode4(De
         page = table[i];
     };
 
-    const Widen<T> widen_k;
-    const Widen<Bf16> widen_v;
+    const Widen<T> widen;
+    const Widen<P> widen_p;
     const float inf = __builtin_inff();
     const float c = a.scale_log2;
     float m = -inf, ref = 0.f, l = 0.f;     // reference, what scores are taken relative to (0 while there is none), sum
@@ -144,7 +165,7 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 3 : 2) void k_attn_decode4(De
             q[g] = Frag{(f[0] & 0xffffu) | f[2] << 16, f[0] >> 16 | (f[2] & 0xffff0000u), (f[1] & 0xffffu) | f[3] << 16,
                         f[1] >> 16 | (f[3] & 0xffff0000u)};
         }
-        if constexpr (kParts == 2) {     // float16: the largest brought to 2^14, so that no part is lost below or above
+        if constexpr (kHalf) {           // float16: the largest brought to 2^14, so that no part is lost below or above
             const int e = top > 0.f && top < __builtin_inff() ? (int)(__float_as_uint(top) >> 23) - 127 - 14 : 0;
             back = __builtin_amdgcn_ldexpf(1.f, e);
 #pragma unroll
@@ -197,7 +218,26 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 3 : 2) void k_attn_decode4(De
         value_at = (pg * a.pg.v.page + (int64_t)place * a.pg.v.token) * 2;
         load(kbase, (pg * a.pg.k.page + (int64_t)place * a.pg.k.token) * 2);
     };
-    auto store = [&](uint64_t live) {
+    float down = 1.f, limit = 0.f;       // what a bfloat16 cache's value steps are scaled with, and what they are below
+    auto raise = [&](float top, const float (&step)[G]) {      // the largest step to 4 .. 8, and with it what there is so far
+        if (top == inf) {
+            top = 0.f;
+#pragma unroll
+            for (int g = 0; g < G; ++g) top = fmaxf(top, fabsf(step[g]) < inf ? fabsf(step[g]) : 0.f);
+            top = max_wave(top);
+            if (top < limit || top == 0.f) return;
+        }
+        const int e = max((int)(__float_as_uint(top) >> 23) - 127, -120);
+        const float next = __builtin_amdgcn_ldexpf(1.f, 2 - e);
+        if (limit > 0.f) {
+            const float less = next / down;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) acc[d] *= less;
+        }
+        down = next;
+        limit = __builtin_amdgcn_ldexpf(2.f, e);
+    };
+    auto store = [&](uint64_t live, bool of_values) {
         const bool there = live >> lane & 1;         // else steps and centres of 0: it counts for nothing
 #pragma unroll
         for (int i = 0; i < MF; ++i) {
@@ -206,11 +246,20 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 3 : 2) void k_attn_decode4(De
                 numbers[i][w] = i * 4 + w < G && there ? numbers[i][w] : 0u;
             *reinterpret_cast<Frag *>(meta + lane * R::kMetaRow + i * 16) = numbers[i];
         }
+        float step[G];
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-            const uint32_t x = numbers[g / 8][g % 8 / 2];
-            steps[g * kChunk + lane] = g % 2 ? high<T>(x) : low<T>(x);
+        for (int g = 0; g < G; ++g) step[g] = g % 2 ? high<T>(numbers[g / 8][g % 8 / 2]) : low<T>(numbers[g / 8][g % 8 / 2]);
+        if (!kHalf && of_values) {
+            float top = 0.f;
+#pragma unroll
+            for (int g = 0; g < G; ++g) top = fmaxf(top, fabsf(step[g]));        // (NaN is left out)
+            top = max_wave(top);
+            if (top >= limit && top > 0.f) raise(top, step);
+#pragma unroll
+            for (int g = 0; g < G; ++g) step[g] *= down;
         }
+#pragma unroll
+        for (int g = 0; g < G; ++g) steps[g * kChunk + lane] = step[g];
 #pragma unroll
         for (int i = 0; i < G; ++i) {
             const int x = i * 64 + lane;
@@ -225,7 +274,7 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 3 : 2) void k_attn_decode4(De
     }
     for (; chunk < to; chunk += kStep) {
         const uint64_t now = live;
-        store(now);
+        store(now, false);
         load(vbase, value_at);
         find(chunk + kStep);
 
@@ -239,7 +288,7 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 3 : 2) void k_attn_decode4(De
             f32x4 x[G];
 #pragma unroll
             for (int g = 0; g < G; ++g)
-                x[g] = T::mfma16(widen_k(*reinterpret_cast<const uint32_t *>(tile + row * R::kRow + g * kGroupBytes + quarter * 4)), q[g], f32x4{});
+                x[g] = T::mfma16(widen(*reinterpret_cast<const uint32_t *>(tile + row * R::kRow + g * kGroupBytes + quarter * 4)), q[g], f32x4{});
             s[t] = side * back;
 #pragma unroll
             for (int g = 0; g < G; ++g) {
@@ -281,19 +330,20 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 3 : 2) void k_attn_decode4(De
         for (int t = 0; t < 4; ++t) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                s[t][i] = exp2_fast(__builtin_fmaf(s[t][i] - ref, c, (float)T::kLift));
+                s[t][i] = exp2_fast(__builtin_fmaf(s[t][i] - ref, c, (float)kLift));
                 l += s[t][i];
             }
         }
 
-        store(now);
+        store(now, true);
         if (chunk + kStep < to) load_keys(chunk + kStep);
 #pragma unroll
         for (int t = 0; t < 4; ++t)
             z = T::mfma16(read_numbers(meta + slot_of(t, quarter * 4 + (col >> 2)) * R::kMetaRow + (col & 3) * 8),
                           u32x2{T::pack(s[t][0], s[t][1]), T::pack(s[t][2], s[t][3])}, z);
         const uint8_t *transposed = tile + slot_of(col >> 2, quarter * 4 + (col & 3)) * R::kRow;
-        const Frag minus = Frag{0xc1bcc1bcu, 0xc1bcc1bcu, 0xc1bcc1bcu, 0xc1bcc1bcu};     // -47/2
+        constexpr uint32_t minus = kHalf ? 0xc1bcc1bcu : 0xcde0cde0u;     // -47/2
+        const Frag less = Frag{minus, minus, minus, minus};
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             Frag p[kParts][2];
@@ -303,9 +353,8 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 3 : 2) void k_attn_decode4(De
                 const f32x4 v = s[y * 2 + 1] * *reinterpret_cast<const f32x4 *>(steps + g * kChunk + slot_of(y * 2 + 1, quarter * 4));
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    p[0][y][i] = Bf16::pack(u[i], v[i]);
-                    if constexpr (kParts == 2)
-                        p[1][y][i] = Bf16::pack(u[i] - low<Bf16>(p[0][y][i]), v[i] - high<Bf16>(p[0][y][i]));
+                    p[0][y][i] = P::pack(u[i], v[i]);
+                    if constexpr (kParts == 2) p[1][y][i] = P::pack(u[i] - low<P>(p[0][y][i]), v[i] - high<P>(p[0][y][i]));
                 }
             }
 #pragma unroll
@@ -314,11 +363,11 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 3 : 2) void k_attn_decode4(De
                 f32x4 o = acc[g * 2 + half];
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    const Frag code = widen_v(x[y]);
+                    const Frag code = widen_p(x[y]);
 #pragma unroll
                     for (int n = 0; n < kParts; ++n) {
-                        o = Bf16::mfma16(minus, p[n][y], o);
-                        o = Bf16::mfma16(code, p[n][y], o);
+                        o = P::mfma16(less, p[n][y], o);
+                        o = P::mfma16(code, p[n][y], o);
                     }
                 }
                 acc[g * 2 + half] = o;
@@ -327,7 +376,7 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 3 : 2) void k_attn_decode4(De
     }
 
     // the block's waves joined: lane's column is a head, its registers dims quarter * 4 + i (of z: a record's numbers)
-    constexpr float unit = 1.f / (1 << T::kLift);
+    constexpr float unit = 1.f / (1 << kLift);
     l = sum_halves(sum_quarters(l)) * unit;
     if (quarter == 0) {
         stat[wave][0][col] = m;
@@ -338,7 +387,7 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 3 : 2) void k_attn_decode4(De
     float *mine = reinterpret_cast<float *>(tile);
 #pragma unroll
     for (int d = 0; d < DT; ++d)
-        *reinterpret_cast<f32x4 *>(mine + col * (DIM + 4) + d * 16 + quarter * 4) = (acc[d] + sums[wave][col][G + d / 2]) * unit;
+        *reinterpret_cast<f32x4 *>(mine + col * (DIM + 4) + d * 16 + quarter * 4) = acc[d] * (unit / down) + sums[wave][col][G + d / 2] * unit;
     __syncthreads();
     const int h = threadIdx.x >> 4;          // 16 heads, 16 threads each
     if (h >= heads) return;
@@ -398,7 +447,7 @@ uint64_t up256(uint64_t x) { return (x + 255) / 256 * 256; }
 uint32_t scores_stride(uint32_t max_len) { return (max_len + 63) / 64 * 64; }
 
 constexpr uint32_t kMinSplit = kWaves * kChunk;      // a chunk for every wave
-constexpr uint32_t kManySplit = 1536;
+constexpr uint32_t kManySplit = 768;
 
 }  // namespace
 

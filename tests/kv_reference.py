@@ -8,7 +8,9 @@ Bounds, from the unit roundoffs u32 = 2^-24 and u (2^-8 for bfloat16, 2^-11 for 
                    rounding, which is less; and 32-bit errors of its argument, 8 u32 (|x| + |centre| + 8 step)
   decode           as in attention_reference.py, where a key (code - 15/2) step + centre is summed as (16 + code)
                    and 47/2 apart, so that 55 step + |centre| stands for |k| in the score's error, in dim + 24 sums; weights
-                   are rounded with their slot's step: u sum p step 15/2, and n u32 sum p (55 step + |centre|)
+                   are rounded with their slot's step: u sum p step 15/2, and n u32 sum p (55 step + |centre|). Weights
+                   times steps are float16 numbers times at least 4 2^12 over the largest step: half its spacing is 2^-25,
+                   so n 15/2 2^-39 of the largest step
 """
 import torch
 
@@ -124,6 +126,7 @@ def attend4(q, keys, values, scale):
     lse_tol = rel + 8 * U32 * (lse.abs() + x.abs().max())
     whole = p @ (7.5 * vs + vz.abs())
     out_tol = 1.01 * (UNIT[kind] * (p @ (7.5 * vs)) + UNIT[kind] * out.abs() + 2 * rel * whole + (n + 8) * U32 * (p @ (55 * vs + vz.abs())))
+    out_tol += n * 7.5 * 2.0 ** -39 * vs.max()
     if kind == torch.float16:
         out_tol += 2.0 ** -24
     return out, lse, out_tol, lse_tol

@@ -315,6 +315,37 @@ def test_decode_extreme_records(ibp):
         check(c, q, out, lse, scale=1e-3)
 
 
+@pytest.mark.parametrize("kind", [BF16, F16])
+@pytest.mark.parametrize("falling", [False, True])
+def test_decode_steps_of_all_sizes(ibp, kind, falling):
+    """Values a thousand times larger at one end of a cache than at the other, groups a hundred times larger than others, slots
+    without a step: what the steps are taken relative to changes on the way."""
+    c = Cache(kind, 2, 128, [2000, 300], 32, seed=15)
+    g = torch.Generator().manual_seed(2)
+    for b, n in enumerate(c.lens):
+        slot = torch.arange(n)
+        size = 10.0 ** (4 * slot / n - 2)
+        x = torch.randn(n, 2, 128, generator=g) * (size.flip(0) if falling else size)[:, None, None]
+        x[..., 32:64] *= 100 if kind == BF16 else 0.01
+        x[::7, :, 64:96] = x[::7, :, 64:65]
+        c.values[c.table[b, slot // 32].long(), :, slot % 32] = records_of(x.to(kind).float(), kind)
+    q = queries(c, 4)
+    before = torch.rand(2, 2, 2000)
+    out, lse, after = decode(ibp, c, q, before)
+    check(c, q, out, lse, before, after)
+
+
+def test_decode_infinite_step(ibp):
+    """Of one group in a bfloat16 cache: its columns are not finite, all others as without it."""
+    c = Cache(BF16, 1, 64, [300], 16, seed=16)
+    q = queries(c, 2)
+    clean, _, _ = decode(ibp, c, q)
+    v = c.values.clone()
+    v[c.table[0, 9].long(), 0, 5, 32:34] = torch.tensor([float("inf")], dtype=BF16).view(torch.uint8)
+    out, _, _ = decode(ibp, c, q, values=v.cuda())
+    assert not out[0, :, :32].isfinite().any() and torch.equal(out[0, :, 32:], clean[0, :, 32:])
+
+
 def test_decode_one_workspace_serves_smaller_calls(ibp):
     c = Cache(BF16, 2, 128, [300, 5000, 40], 32, seed=10)
     q = queries(c, 8)
