@@ -76,28 +76,28 @@ __device__ __forceinline__ u32x2 narrow(f32x4 x) {
 // x a + y b, each product and the sum rounded.
 __device__ __forceinline__ float turned(float x, float a, float y, float b) { return x * a + y * b; }
 
-// A head's quad `to` (four values from there on) after turning.
-template <class T>
-__device__ __forceinline__ f32x4 turned_quad(const Append &a, const uint8_t *head, const float *angles, uint32_t to) {
-    const f32x4 x = widen<T>(*reinterpret_cast<const u32x2 *>(head + to * 2));
-    if (to >= a.turned) return x;
-    const uint32_t half = a.turned / 2;
-    f32x4 o;
-    if (a.halves) {
-        const bool second = to >= half;
-        const uint32_t pair = second ? to - half : to;
-        const f32x4 y = widen<T>(*reinterpret_cast<const u32x2 *>(head + (second ? pair : to + half) * 2));
-        const f32x4 *cs = reinterpret_cast<const f32x4 *>(angles + pair * 2);
-        const f32x4 c0 = cs[0], c1 = cs[1];
-        const f32x4 c = {c0[0], c0[2], c1[0], c1[2]}, s = {c0[1], c0[3], c1[1], c1[3]};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = second ? turned(y[i], s[i], x[i], c[i]) : turned(x[i], c[i], -y[i], s[i]);
-    } else {
-        const f32x4 cs = *reinterpret_cast<const f32x4 *>(angles + to);
-        o = f32x4{turned(x[0], cs[0], -x[1], cs[1]), turned(x[0], cs[1], x[1], cs[0]),
-                  turned(x[2], cs[2], -x[3], cs[3]), turned(x[2], cs[3], x[3], cs[2])};
-    }
-    return o;
+// Cosines and sines of four pairs.
+struct Angles {
+    f32x4 c, s;
+};
+__device__ __forceinline__ Angles angles_at(const float *p) {
+    const f32x4 x = *reinterpret_cast<const f32x4 *>(p), y = *reinterpret_cast<const f32x4 *>(p + 4);
+    return Angles{f32x4{x[0], x[2], y[0], y[2]}, f32x4{x[1], x[3], y[1], y[3]}};
+}
+__device__ __forceinline__ f32x4 first_of(f32x4 x, f32x4 y, const Angles &a) {
+    return f32x4{turned(x[0], a.c[0], -y[0], a.s[0]), turned(x[1], a.c[1], -y[1], a.s[1]), turned(x[2], a.c[2], -y[2], a.s[2]),
+                 turned(x[3], a.c[3], -y[3], a.s[3])};
+}
+__device__ __forceinline__ f32x4 second_of(f32x4 x, f32x4 y, const Angles &a) {
+    return f32x4{turned(x[0], a.s[0], y[0], a.c[0]), turned(x[1], a.s[1], y[1], a.c[1]), turned(x[2], a.s[2], y[2], a.c[2]),
+                 turned(x[3], a.s[3], y[3], a.c[3])};
+}
+// Eight values, four pairs of neighbours.
+__device__ __forceinline__ void turn_neighbours(f32x4 &u, f32x4 &v, const Angles &a) {
+    const f32x4 x = {u[0], u[2], v[0], v[2]}, y = {u[1], u[3], v[1], v[3]};
+    const f32x4 p = first_of(x, y, a), q = second_of(x, y, a);
+    u = f32x4{p[0], q[0], p[1], q[1]};
+    v = f32x4{p[2], q[2], p[3], q[3]};
 }
 
 // Eight values of a head, in the lanes of its group of 32 (four in a row), as their dword of codes; step and centre.
@@ -136,96 +136,207 @@ __device__ __forceinline__ uint32_t codes_of(const float *x, uint32_t there, uin
     return there < 8 ? code & (there ? 0xffffffffu >> (32 - 4 * there) : 0u) : code;
 }
 
-// A block per row; a thread takes eight values of a head at a time, `octs` (a power of two, at least
-// the head's) threads per head.
-template <class T, bool FOUR>
-__global__ __launch_bounds__(kThreads) void k_kv_append(Append a, uint32_t octs_log2) {
-    const uint32_t row = blockIdx.x;
+// What a row's wave needs of its sequence. Asked for behind the loads of the row's values, which need none of it.
+struct Where {
     uint32_t seq;
-    int back;
-    if (!find_row(a.starts, a.n_seqs, a.rows, row, seq, back)) return;
-    const int64_t slot = (int64_t)a.lens[seq] - back, position = (int64_t)a.next[seq] - back;
-    const float *angles = a.rotation + min(max(position, (int64_t)0), (int64_t)a.positions - 1) * a.turned;
+    int64_t slot, position;
     Place place;
-    const bool there = find_slot(a.pg, seq, slot, place);
-    const uint32_t heads = a.q_heads + 2 * a.kv_heads, octs = 1u << octs_log2, half = a.turned / 2;
-    for (uint32_t item = threadIdx.x; item < heads << octs_log2; item += kThreads) {
-        const uint32_t h = item >> octs_log2, oct = item & (octs - 1), d = oct * 8;
-        const bool is_q = h < a.q_heads, is_k = !is_q && h < a.q_heads + a.kv_heads;
-        const uint32_t head = is_q ? h : is_k ? h - a.q_heads : h - a.q_heads - a.kv_heads;
-        const Rows &in = is_q ? a.q : is_k ? a.k : a.v;
-        const uint8_t *from = (const uint8_t *)in.data + ((int64_t)row * in.row + (int64_t)head * in.head) * 2;
-        if (!is_q && !there) continue;
-        if (FOUR && !is_q) {
-            const uint32_t groups = record_groups(a.dim);
-            if (d >= groups * kGroupValues) continue;
-            const uint32_t have = min(max((int)a.dim - (int)d, 0), 8);
-            float x[8] = {};
+    bool there;
+    const float *angles;
+};
+__device__ __forceinline__ bool find_where(const Append &a, uint32_t row, Where &w) {
+    int back;
+    if (!find_row(a.starts, a.n_seqs, a.rows, row, w.seq, back)) return false;
+    w.slot = (int64_t)a.lens[w.seq] - back;
+    w.position = (int64_t)a.next[w.seq] - back;
+    w.angles = a.rotation + min(max(w.position, (int64_t)0), (int64_t)a.positions - 1) * a.turned;
+    w.there = find_slot(a.pg, w.seq, w.slot, w.place);
+    return true;
+}
+
+// Items, of eight values each, that a lane has on their way together: four fill the chip's memory system, and in calls of too few
+// rows for that one each is sooner done.
+constexpr int kMany = 4;
+constexpr uint64_t kFewWaves = 2048;     // (of four items)
+
+// Waves are shared out as `parts` per row: each takes 64 N items of its heads, first of those that stay 16 bits wide (`wide`
+// parts: queries, and without FOUR keys and values), then of those that are held in 4. A lane's items are the same eight
+// values of several heads, `octs` (a power of two, at least the head's) lanes per head, so that it needs the angles once.
+template <class T, bool FOUR, int N>
+__global__ __launch_bounds__(kThreads) void k_kv_append(Append a, uint32_t wide_log2, uint32_t four_log2, uint32_t wide, uint32_t parts) {
+    const uint32_t wave = (uint32_t)uniform((int)(blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6)));
+    const uint32_t row = wave / parts, part = wave - row * parts, lane = threadIdx.x & 63;
+    if (row >= a.rows) return;
+    const uint32_t half = a.turned / 2;
+    Where w;
+    if (part < wide) {
+        const uint32_t heads = a.q_heads + (FOUR ? 0 : 2 * a.kv_heads), oct = lane & ((1u << wide_log2) - 1), d = oct * 8;
+        const uint32_t head0 = ((part * N * 64) + lane) >> wide_log2, head_step = 64u >> wide_log2;
+        // both quads of four pairs, so that nothing that another lane writes is read: queries may be turned in place
+        const bool turn = d < a.turned, apart = turn && a.halves;
+        const uint32_t q0 = apart ? oct * 4 : d, q1 = apart ? half + oct * 4 : d + 4;
+        u32x2 x[N], y[N];
+        auto in_heads = [&](int n, uint32_t &head, uint32_t &which) {
+            const uint32_t h = head0 + n * head_step;
+            which = h < a.q_heads ? 0 : h < a.q_heads + a.kv_heads ? 1 : 2;
+            head = which == 0 ? h : which == 1 ? h - a.q_heads : h - a.q_heads - a.kv_heads;
+            return h < heads && d < a.dim;
+        };
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            uint32_t head, which;
+            if (!in_heads(n, head, which)) continue;
+            const Rows &in = which == 0 ? a.q : which == 1 ? a.k : a.v;
+            const bool mixed = which != 2;
+            const uint8_t *from = (const uint8_t *)in.data + ((int64_t)row * in.row + (int64_t)head * in.head) * 2;
+            x[n] = *reinterpret_cast<const u32x2 *>(from + (mixed ? q0 : d) * 2);
+            y[n] = *reinterpret_cast<const u32x2 *>(from + (mixed ? q1 : d + 4) * 2);
+        }
+        if (!find_where(a, row, w)) return;
+        Angles at{};
+        if (turn) at = angles_at(w.angles + oct * 8);
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            uint32_t head, which;
+            if (!in_heads(n, head, which) || (which != 0 && !w.there)) continue;
+            const bool mixed = which != 2;
+            uint8_t *to = which == 0 ? (uint8_t *)a.q_out.data + ((int64_t)row * a.q_out.row + (int64_t)head * a.q_out.head) * 2
+                                     : at_slot(which == 1 ? a.pg.k : a.pg.v, w.place, head);
+            if (mixed && turn) {
+                f32x4 u = widen<T>(x[n]), v = widen<T>(y[n]);
+                if (a.halves) {
+                    const f32x4 p = first_of(u, v, at);
+                    v = second_of(u, v, at);
+                    u = p;
+                } else {
+                    turn_neighbours(u, v, at);
+                }
+                x[n] = narrow<T>(u);
+                y[n] = narrow<T>(v);
+            }
+            *reinterpret_cast<u32x2 *>(to + (mixed ? q0 : d) * 2) = x[n];
+            *reinterpret_cast<u32x2 *>(to + (mixed ? q1 : d + 4) * 2) = y[n];
+        }
+    } else if constexpr (FOUR) {
+        const uint32_t groups = record_groups(a.dim), oct = lane & ((1u << four_log2) - 1), d = oct * 8;
+        const uint32_t head0 = (((part - wide) * N * 64) + lane) >> four_log2, head_step = 64u >> four_log2;
+        const uint32_t have = min(max((int)a.dim - (int)d, 0), 8);
+        const bool turn = d < a.turned;
+        // of pairs that are apart the other quads
+        uint32_t other[2], pair[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t at = d + 4 * i;
+            other[i] = at < half ? at + half : at - half;
+            pair[i] = at < half ? at : at - half;
+        }
+        u32x2 x[N][2], y[N][2];
+        auto in_heads = [&](int n, uint32_t &head, bool &is_k) {
+            const uint32_t h = head0 + n * head_step;
+            is_k = h < a.kv_heads;
+            head = is_k ? h : h - a.kv_heads;
+            return h < 2 * a.kv_heads && oct < groups * 4;
+        };
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            uint32_t head;
+            bool is_k;
+            if (!in_heads(n, head, is_k) || !have) continue;
+            const Rows &in = is_k ? a.k : a.v;
+            const uint8_t *from = (const uint8_t *)in.data + ((int64_t)row * in.row + (int64_t)head * in.head) * 2;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) x[n][i] = *reinterpret_cast<const u32x2 *>(from + (d + 4 * i) * 2);
+            if (is_k && turn && a.halves) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) y[n][i] = *reinterpret_cast<const u32x2 *>(from + other[i] * 2);
+            }
+        }
+        if (!find_where(a, row, w) || !w.there) return;
+        Angles at[2]{};
+        if (turn) {
+            if (a.halves) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) at[i] = angles_at(w.angles + pair[i] * 2);
+            } else {
+                at[0] = angles_at(w.angles + d);
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            uint32_t head;
+            bool is_k;
+            if (!in_heads(n, head, is_k)) continue;
+            f32x4 u{}, v{};
             if (have) {
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    const f32x4 v = is_k ? turned_quad<T>(a, from, angles, d + 4 * y) : widen<T>(*reinterpret_cast<const u32x2 *>(from + (d + 4 * y) * 2));
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) x[4 * y + i] = v[i];
+                u = widen<T>(x[n][0]);
+                v = widen<T>(x[n][1]);
+                if (is_k && turn) {
+                    if (a.halves) {
+                        const f32x4 p = widen<T>(y[n][0]), q = widen<T>(y[n][1]);
+                        u = d < half ? first_of(u, p, at[0]) : second_of(p, u, at[0]);
+                        v = d + 4 < half ? first_of(v, q, at[1]) : second_of(q, v, at[1]);
+                    } else {
+                        turn_neighbours(u, v, at[0]);
+                    }
                 }
             }
+            const float z[8] = {u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
             uint16_t step, centre;
-            const uint32_t code = codes_of<T>(x, have, step, centre);
-            uint8_t *to = at_slot(is_k ? a.pg.k : a.pg.v, place, head);
+            const uint32_t code = codes_of<T>(z, have, step, centre);
+            uint8_t *to = at_slot(is_k ? a.pg.k : a.pg.v, w.place, head);
             *reinterpret_cast<uint32_t *>(to + oct * 4) = code;
             if ((oct & 3) == 0) {
                 uint8_t *meta = to + groups * kGroupBytes + oct / 4 * 2;
                 *reinterpret_cast<uint16_t *>(meta) = step;
                 *reinterpret_cast<uint16_t *>(meta + groups * 2) = centre;
             }
-            continue;
         }
-        if (d >= a.dim) continue;
-        uint8_t *to = is_q ? (uint8_t *)a.q_out.data + ((int64_t)row * a.q_out.row + (int64_t)head * a.q_out.head) * 2
-                           : at_slot(is_k ? a.pg.k : a.pg.v, place, head);
-        if (h >= a.q_heads + a.kv_heads || d >= a.turned) {
-            *reinterpret_cast<Frag *>(to + d * 2) = *reinterpret_cast<const Frag *>(from + d * 2);
-            continue;
-        }
-        // both quads of four pairs: nothing that another thread writes is read, so that queries may be turned in place
-        const uint32_t q0 = a.halves ? oct * 4 : d, q1 = a.halves ? half + oct * 4 : d + 4;
-        const f32x4 x = turned_quad<T>(a, from, angles, q0), y = turned_quad<T>(a, from, angles, q1);
-        *reinterpret_cast<u32x2 *>(to + q0 * 2) = narrow<T>(x);
-        *reinterpret_cast<u32x2 *>(to + q1 * 2) = narrow<T>(y);
     }
-    if (there && a.weights && slot < (int64_t)a.stride)
-        for (uint32_t h = threadIdx.x; h < a.kv_heads; h += kThreads) {
-            a.weights[((int64_t)seq * a.kv_heads + h) * a.stride + slot] = 0.f;
-        }
-    if (there && a.places && slot < (int64_t)a.stride)
-        for (uint32_t h = threadIdx.x; h < a.kv_heads; h += kThreads)
-            a.places[((int64_t)seq * a.kv_heads + h) * a.stride + slot] = (int32_t)position;
+    if (part != parts - 1 || !w.there || w.slot >= (int64_t)a.stride) return;
+    const int64_t at = (int64_t)w.seq * a.kv_heads * a.stride + w.slot;
+    for (uint32_t h = lane; h < a.kv_heads; h += 64) {
+        if (a.weights) a.weights[at + h * a.stride] = 0.f;
+        if (a.places) a.places[at + h * a.stride] = (int32_t)w.position;
+    }
 }
 
-// A block per row, threads as above.
-template <class T>
-__global__ __launch_bounds__(kThreads) void k_kv4_read(Read4 a, uint32_t octs_log2) {
-    const uint32_t row = blockIdx.x;
+// The same shares of a row; a lane's values are the same eight of several heads.
+template <class T, int N>
+__global__ __launch_bounds__(kThreads) void k_kv4_read(Read4 a, uint32_t octs_log2, uint32_t parts) {
+    const uint32_t wave = (uint32_t)uniform((int)(blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6)));
+    const uint32_t row = wave / parts, part = wave - row * parts, lane = threadIdx.x & 63;
+    if (row >= a.rows) return;
     uint32_t seq;
     int back;
     if (!find_row(a.starts, a.n_seqs, a.rows, row, seq, back)) return;
     const int64_t slot = (a.first ? (int64_t)a.first[seq] : 0) + (a.starts ? (int64_t)row - a.starts[seq] : 0);
     Place place;
     if (slot >= a.lens[seq] || !find_slot(a.pg, seq, slot, place)) return;
-    const uint32_t octs = 1u << octs_log2, groups = record_groups(a.dim);
-    for (uint32_t item = threadIdx.x; item < 2 * a.kv_heads << octs_log2; item += kThreads) {
-        const uint32_t h = item >> octs_log2, oct = item & (octs - 1), d = oct * 8;
-        if (d >= a.dim) continue;
+    const uint32_t groups = record_groups(a.dim), oct = lane & ((1u << octs_log2) - 1), d = oct * 8;
+    const uint32_t head0 = ((part * N * 64) + lane) >> octs_log2, head_step = 64u >> octs_log2;
+    if (d >= a.dim) return;
+    uint32_t code[N];
+    uint16_t step[N], centre[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const uint32_t h = min(head0 + n * head_step, 2 * a.kv_heads - 1);
         const bool is_k = h < a.kv_heads;
-        const uint32_t head = is_k ? h : h - a.kv_heads;
-        const uint8_t *from = at_slot(is_k ? a.pg.k : a.pg.v, place, head), *meta = from + groups * kGroupBytes + oct / 4 * 2;
+        const uint8_t *from = at_slot(is_k ? a.pg.k : a.pg.v, place, is_k ? h : h - a.kv_heads), *meta = from + groups * kGroupBytes + oct / 4 * 2;
+        code[n] = *reinterpret_cast<const uint32_t *>(from + oct * 4);
+        step[n] = *reinterpret_cast<const uint16_t *>(meta);
+        centre[n] = *reinterpret_cast<const uint16_t *>(meta + groups * 2);
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const uint32_t h = head0 + n * head_step;
+        if (h >= 2 * a.kv_heads) return;
+        const bool is_k = h < a.kv_heads;
         const Rows &out = is_k ? a.k : a.v;
-        const uint32_t code = *reinterpret_cast<const uint32_t *>(from + oct * 4);
-        const float step = T::value(*reinterpret_cast<const uint16_t *>(meta)), centre = T::value(*reinterpret_cast<const uint16_t *>(meta + groups * 2));
+        const float s = T::value(step[n]), c = T::value(centre[n]);
         float x[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf((float)(code >> 4 * i & 15) - 7.5f, step, centre);
-        *reinterpret_cast<Frag *>((uint8_t *)out.data + ((int64_t)row * out.row + (int64_t)head * out.head + d) * 2) =
+        for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf((float)(code[n] >> 4 * i & 15) - 7.5f, s, c);
+        *reinterpret_cast<Frag *>((uint8_t *)out.data + ((int64_t)row * out.row + (int64_t)(is_k ? h : h - a.kv_heads) * out.head + d) * 2) =
             Frag{T::pack(x[0], x[1]), T::pack(x[2], x[3]), T::pack(x[4], x[5]), T::pack(x[6], x[7])};
     }
 }
@@ -236,30 +347,53 @@ uint32_t log2_up(uint32_t x) {
     return n;
 }
 
+// Waves of `items` items a lane that `heads` heads of 2^octs_log2 of them make.
+uint64_t parts_of(uint64_t heads, uint32_t octs_log2, int items) { return ((heads << octs_log2) + 64 * items - 1) / (64 * items); }
+
+// A row's parts times the rows, as blocks; 0: more than a launch has.
+uint32_t blocks_of(uint64_t rows, uint64_t parts) {
+    const uint64_t blocks = (rows * parts + kThreads / 64 - 1) / (kThreads / 64);
+    return blocks > kMaxGrid || rows > kMaxGrid ? 0 : (uint32_t)blocks;
+}
+
 }  // namespace
 
 hipError_t launch_append(const Append &a, hipStream_t stream) {
     if (a.rows == 0 || a.n_seqs == 0) return hipSuccess;
-    if (a.rows > kMaxGrid) return hipErrorInvalidConfiguration;
-    const uint32_t octs = log2_up(a.four ? record_groups(a.dim) * 4 : a.dim / 8);
-    const dim3 grid(a.rows), block(kThreads);
-    if (a.f16) {
-        if (a.four) k_kv_append<F16, true><<<grid, block, 0, stream>>>(a, octs);
-        else k_kv_append<F16, false><<<grid, block, 0, stream>>>(a, octs);
-    } else {
-        if (a.four) k_kv_append<Bf16, true><<<grid, block, 0, stream>>>(a, octs);
-        else k_kv_append<Bf16, false><<<grid, block, 0, stream>>>(a, octs);
-    }
-    return hipGetLastError();
+    const uint32_t wide_log2 = log2_up(a.dim / 8), four_log2 = log2_up(record_groups(a.dim) * 4);
+    const uint64_t wide_heads = a.q_heads + (a.four ? 0ull : 2ull * a.kv_heads), four_heads = a.four ? 2ull * a.kv_heads : 0;
+    auto launch = [&](auto kernel, int items) {
+        const uint64_t wide = parts_of(wide_heads, wide_log2, items), parts = wide + parts_of(four_heads, four_log2, items);
+        const uint32_t blocks = blocks_of(a.rows, parts);
+        if (!blocks) return hipErrorInvalidConfiguration;
+        kernel<<<dim3(blocks), dim3(kThreads), 0, stream>>>(a, wide_log2, four_log2, (uint32_t)wide, (uint32_t)parts);
+        return hipGetLastError();
+    };
+    const bool many = a.rows * (parts_of(wide_heads, wide_log2, kMany) + parts_of(four_heads, four_log2, kMany)) >= kFewWaves;
+    auto of_type = [&](auto type) {
+        using T = decltype(type);
+        if (many) return launch(a.four ? k_kv_append<T, true, kMany> : k_kv_append<T, false, kMany>, kMany);
+        return launch(a.four ? k_kv_append<T, true, 1> : k_kv_append<T, false, 1>, 1);
+    };
+    return a.f16 ? of_type(F16{}) : of_type(Bf16{});
 }
 
 hipError_t launch_read4(const Read4 &r, hipStream_t stream) {
     if (r.rows == 0 || r.n_seqs == 0) return hipSuccess;
-    if (r.rows > kMaxGrid) return hipErrorInvalidConfiguration;
     const uint32_t octs = log2_up(r.dim / 8);
-    if (r.f16) k_kv4_read<F16><<<dim3(r.rows), dim3(kThreads), 0, stream>>>(r, octs);
-    else k_kv4_read<Bf16><<<dim3(r.rows), dim3(kThreads), 0, stream>>>(r, octs);
-    return hipGetLastError();
+    auto launch = [&](auto kernel, int items) {
+        const uint64_t parts = parts_of(2ull * r.kv_heads, octs, items);
+        const uint32_t blocks = blocks_of(r.rows, parts);
+        if (!blocks) return hipErrorInvalidConfiguration;
+        kernel<<<dim3(blocks), dim3(kThreads), 0, stream>>>(r, octs, (uint32_t)parts);
+        return hipGetLastError();
+    };
+    auto of_type = [&](auto type) {
+        using T = decltype(type);
+        if (r.rows * parts_of(2ull * r.kv_heads, octs, kMany) >= kFewWaves) return launch(k_kv4_read<T, kMany>, kMany);
+        return launch(k_kv4_read<T, 1>, 1);
+    };
+    return r.f16 ? of_type(F16{}) : of_type(Bf16{});
 }
 
 }  // namespace attn
