@@ -34,102 +34,127 @@ SIGS = {
 for _f, _args in SIGS.items():
     getattr(lib(), _f).argtypes = _args
     getattr(lib(), _f).restype = ctypes.c_int
+_KV_APPEND, _KV4_APPEND, _KV4_READ, _DECODE4 = (getattr(lib(), f) for f in ("ibp_kv_append", "ibp_kv4_append", "ibp_kv4_read", "ibp_attn_decode4"))
+
+# A step of a serving loop is a few microseconds on the GPU, and a call's checks count beside that: _rows_of, _pool_of and _numbers
+# pass what is in order at once, and leave the rest to the functions that say what is wrong.
+
+
+def _rows_of(x, what, kind, device, heads=None, dim=None):
+    if isinstance(x, torch.Tensor) and x.dtype is kind and x.get_device() == device and x.dim() == 3:
+        n, h, d = x.shape
+        a, b, c = x.stride()
+        if c == 1 and (heads is None or h == heads) and (dim is None or d == dim):
+            return ibp_rows(x.data_ptr(), n, a if n > 1 else 0, b if h > 1 else 0)
+    return _rows(x, what, kind, device, heads, dim)
+
+
+def _numbers(x, what, kind, device, shape):
+    """Address of a contiguous tensor of one type and shape."""
+    if isinstance(x, torch.Tensor) and x.dtype is kind and x.get_device() == device and x.is_contiguous() and x.shape == shape:
+        return x.data_ptr()
+    return _array(x, what, kind, device, shape)
 
 
 def _pool_of(keys, values, table, device, kind, unit, kv_heads, width, what):
     """Pools [n_pages][kv_heads][page_tokens][width] of one kind; unit: elements of it in 2 bytes."""
+    if not (isinstance(keys, torch.Tensor) and isinstance(values, torch.Tensor) and keys.dtype is kind and values.dtype is kind
+            and keys.get_device() == device and values.get_device() == device and keys.dim() == 4 and keys.shape == values.shape):
+        _wrong_pools(keys, values, device, kind, kv_heads, width, what)
+    n, h, t, w = keys.shape
+    if h != kv_heads or w != width:
+        _wrong_pools(keys, values, device, kind, kv_heads, width, what)
+    a, b, c, d = keys.stride()
+    e, f, g, i = values.stride()
+    if d != 1 or i != 1:
+        raise TypeError("keys and values: the last dimension must be contiguous")
+    if n == 1 or h == 1 or t == 1:                   # (a dimension of one has no stride)
+        a, e = (a, e) if n > 1 else (0, 0)
+        b, f = (b, f) if h > 1 else (0, 0)
+        c, g = (c, g) if t > 1 else (0, 0)
+    if (a | b | c | e | f | g) & (8 * unit - 1):
+        raise ValueError("keys and values: strides must be multiples of 16 bytes")
+    table_at = _array(table, "table", torch.int32, device)
+    if table.dim() != 2:
+        raise ValueError("table must be [sequences][pages]")
+    if unit == 2:
+        a, b, c, e, f, g = a >> 1, b >> 1, c >> 1, e >> 1, f >> 1, g >> 1
+    return ibp_pages(keys.data_ptr(), values.data_ptr(), n, t, table.shape[1], table_at, a, b, c, e, f, g)
+
+
+def _wrong_pools(keys, values, device, kind, kv_heads, width, what):
     for x, name in ((keys, "keys"), (values, "values")):
         _tensor(x, name, device)
         if x.dtype != kind:
             raise TypeError(f"{name} must be {kind}, not {x.dtype}")
         if x.dim() != 4 or x.shape[1] != kv_heads or x.shape[3] != width:
             raise ValueError(f"{name} must be [n_pages][{kv_heads}][page_tokens][{width}] ({what}), not {list(x.shape)}")
-    if keys.shape != values.shape:
-        raise ValueError("keys and values must have the same shape")
-    table_at = _array(table, "table", torch.int32, device)
-    if table.dim() != 2:
-        raise ValueError("table must be [sequences][pages]")
-    n, h, t, w = keys.shape
-    strides = []
-    for x, name in ((keys, "keys"), (values, "values")):
-        s = x.stride()
-        if s[3] != 1 and w != 1:
-            raise TypeError(f"{name}: the last dimension must be contiguous")
-        for size, stride in zip((n, h, t), s):
-            if size > 1 and stride % (8 * unit):
-                raise ValueError(f"{name}: strides must be multiples of 16 bytes")
-            strides.append(stride // unit if size > 1 else 0)
-    return ibp_pages(keys.data_ptr(), values.data_ptr(), n, t, table.shape[1], table_at, *strides)
+    raise ValueError("keys and values must have the same shape")
 
 
 def _sequences(table, lens, starts, rows, device):
     """Their number, and the addresses of their lengths and starts."""
     n = table.shape[0]
-    lens_at = _array(lens, "lens", torch.int32, device, (n,))
+    lens_at = _numbers(lens, "lens", torch.int32, device, (n,))
     if starts is None:
         if rows != n:
             raise ValueError("without starts every sequence has one row")
         return n, lens_at, None
-    return n, lens_at, _array(starts, "starts", torch.int32, device, (n + 1,))
+    return n, lens_at, _numbers(starts, "starts", torch.int32, device, (n + 1,))
 
 
-def _append_to(call, four, k, v, keys, values, table, lens, next_positions, starts, rotation, halves, q, q_out, weights, positions,
-               stream):
-    device = _device(k, "k")
-    kind = k.dtype
-    if kind not in TYPES:
-        raise TypeError(f"k must be bfloat16 or float16, not {kind}")
-    rk = _rows(k, "k", kind, device)
-    rows, kv_heads, dim = k.shape
-    rv = _rows(v, "v", kind, device, kv_heads, dim)
-    if four:
-        pages = _pool_of(keys, values, table, device, torch.uint8, 2, kv_heads, ibp_kv4_record(dim), "records")
-    else:
-        pages = _pool_of(keys, values, table, device, kind, 1, kv_heads, dim, "values")
-    n, lens_at, starts_at = _sequences(table, lens, starts, rows, device)
-    next_at = lens_at if next_positions is lens else _array(next_positions, "next_positions", torch.int32, device, (n,))
-    rq = ro = turn = None
-    heads = kv_heads
-    if q is not None:
-        rq = _rows(q, "q", kind, device)
-        heads = q.shape[1]
-        ro = rq if q_out is None or q_out is q else _rows(q_out, "q_out", kind, device, heads, dim)
-        if q.shape[2] != dim:
-            raise ValueError(f"q must have heads of {dim}, not {q.shape[2]}")
-    elif q_out is not None:
-        raise ValueError("q_out without q")
-    if rotation is not None:
-        at = _array(rotation, "rotation", torch.float32, device)
-        if rotation.dim() != 3 or rotation.shape[2] != 2:
-            raise ValueError("rotation must be [positions][pairs][2]")
-        turn = ibp_rotation(at, rotation.shape[0], 2 * rotation.shape[1], bool(halves))
-    slots, weights_at, positions_at = 0, None, None
-    for x, what, t in ((weights, "weights", torch.float32), (positions, "positions", torch.int32)):
-        if x is None:
-            continue
-        at = _array(x, what, t, device)
-        if x.dim() != 3 or x.shape[0] != n or x.shape[1] != kv_heads or slots not in (0, x.shape[2]):
-            raise ValueError("weights and positions must be [sequences][kv_heads][slots]")
-        slots = x.shape[2]
-        if what == "weights":
-            weights_at = at
+def _appender(call, name, four, about):
+    def append(k, v, keys, values, table, lens, next_positions, starts=None, rotation=None, halves=True, q=None, q_out=None, weights=None,
+               positions=None, stream=None):
+        device = _device(k, "k")
+        kind = k.dtype
+        if kind not in TYPES:
+            raise TypeError(f"k must be bfloat16 or float16, not {kind}")
+        rk = _rows_of(k, "k", kind, device)
+        rows, kv_heads, dim = k.shape
+        rv = _rows_of(v, "v", kind, device, kv_heads, dim)
+        if four:
+            pages = _pool_of(keys, values, table, device, torch.uint8, 2, kv_heads, ibp_kv4_record(dim), "records")
         else:
-            positions_at = at
-    a = ibp_attn(TYPES[kind], heads, kv_heads, dim, 1.0, 0)
-    check(getattr(lib(), call)(a, rk, rv, rq, ro, turn, starts_at, n, pages, lens_at, next_at, weights_at, positions_at, slots,
-                               _stream(stream, device)), call)
+            pages = _pool_of(keys, values, table, device, kind, 1, kv_heads, dim, "values")
+        n, lens_at, starts_at = _sequences(table, lens, starts, rows, device)
+        next_at = lens_at if next_positions is lens else _numbers(next_positions, "next_positions", torch.int32, device, (n,))
+        rq = ro = turn = None
+        heads = kv_heads
+        if q is not None:
+            rq = _rows_of(q, "q", kind, device, None, dim)
+            heads = q.shape[1]
+            ro = rq if q_out is None or q_out is q else _rows_of(q_out, "q_out", kind, device, heads, dim)
+        elif q_out is not None:
+            raise ValueError("q_out without q")
+        if rotation is not None:
+            at = _array(rotation, "rotation", torch.float32, device)
+            shape = rotation.shape
+            if len(shape) != 3 or shape[2] != 2:
+                raise ValueError("rotation must be [positions][pairs][2]")
+            turn = ibp_rotation(at, shape[0], 2 * shape[1], 1 if halves else 0)
+        slots, weights_at, positions_at = 0, None, None
+        if weights is not None:
+            weights_at, slots = _tracked(weights, "weights", torch.float32, device, n, kv_heads, None)
+        if positions is not None:
+            positions_at, slots = _tracked(positions, "positions", torch.int32, device, n, kv_heads, slots if weights is not None else None)
+        a = ibp_attn(TYPES[kind], heads, kv_heads, dim, 1.0, 0)
+        status = call(a, rk, rv, rq, ro, turn, starts_at, n, pages, lens_at, next_at, weights_at, positions_at, slots,
+                      _stream(stream, device))
+        if status:
+            check(status, name)
+
+    append.__name__ = append.__qualname__ = name
+    append.__doc__ = about
+    return append
 
 
-def ibp_kv_append(k, v, keys, values, table, lens, next_positions, starts=None, rotation=None, halves=True, q=None, q_out=None,
-                  weights=None, positions=None, stream=None):
-    """Rows of k and v [rows][kv_heads][dim] become the last slots of their sequences in the pools keys and
-    values [n_pages][kv_heads][page_tokens][dim], keys turned by their positions. starts (int32
-    [sequences + 1]): where each sequence's rows begin; None: one row each. lens and next_positions (int32)
-    are those after the call, and may be one tensor. rotation: float32 [positions][pairs][2], cosine and sine;
-    halves: pairs are (i, i + pairs), else (2 i, 2 i + 1). q [rows][q_heads][dim] is turned into q_out (None: in
-    place). weights (float32) and positions (int32) [sequences][kv_heads][slots] get 0 and the position."""
-    _append_to("ibp_kv_append", False, k, v, keys, values, table, lens, next_positions, starts, rotation, halves, q, q_out, weights,
-               positions, stream)
+def _tracked(x, what, kind, device, n, kv_heads, slots):
+    at = _array(x, what, kind, device)
+    shape = x.shape
+    if len(shape) != 3 or shape[0] != n or shape[1] != kv_heads or (slots is not None and shape[2] != slots):
+        raise ValueError("weights and positions must be [sequences][kv_heads][slots]")
+    return at, shape[2]
 
 
 _records = {}
@@ -145,11 +170,13 @@ def ibp_kv4_record(head_dim):
     return got
 
 
-def ibp_kv4_append(k, v, keys, values, table, lens, next_positions, starts=None, rotation=None, halves=True, q=None, q_out=None,
-                   weights=None, positions=None, stream=None):
-    """ibp_kv_append into pools of 4-bit records, uint8 [n_pages][kv_heads][page_tokens][ibp_kv4_record(dim)]."""
-    _append_to("ibp_kv4_append", True, k, v, keys, values, table, lens, next_positions, starts, rotation, halves, q, q_out, weights,
-               positions, stream)
+ibp_kv_append = _appender(_KV_APPEND, "ibp_kv_append", False, """Rows of k and v [rows][kv_heads][dim] become the last slots of their sequences in the pools keys and
+    values [n_pages][kv_heads][page_tokens][dim], keys turned by their positions. starts (int32
+    [sequences + 1]): where each sequence's rows begin; None: one row each. lens and next_positions (int32)
+    are those after the call, and may be one tensor. rotation: float32 [positions][pairs][2], cosine and sine;
+    halves: pairs are (i, i + pairs), else (2 i, 2 i + 1). q [rows][q_heads][dim] is turned into q_out (None: in
+    place). weights (float32) and positions (int32) [sequences][kv_heads][slots] get 0 and the position.""")
+ibp_kv4_append = _appender(_KV4_APPEND, "ibp_kv4_append", True, """ibp_kv_append into pools of 4-bit records, uint8 [n_pages][kv_heads][page_tokens][ibp_kv4_record(dim)].""")
 
 
 def ibp_kv4_read(keys, values, table, lens, k, v, starts=None, first=None, stream=None):
@@ -159,14 +186,16 @@ def ibp_kv4_read(keys, values, table, lens, k, v, starts=None, first=None, strea
     kind = k.dtype
     if kind not in TYPES:
         raise TypeError(f"k must be bfloat16 or float16, not {kind}")
-    rk = _rows(k, "k", kind, device)
+    rk = _rows_of(k, "k", kind, device)
     rows, kv_heads, dim = k.shape
-    rv = _rows(v, "v", kind, device, kv_heads, dim)
+    rv = _rows_of(v, "v", kind, device, kv_heads, dim)
     pages = _pool_of(keys, values, table, device, torch.uint8, 2, kv_heads, ibp_kv4_record(dim), "records")
     n, lens_at, starts_at = _sequences(table, lens, starts, rows, device)
-    first_at = None if first is None else _array(first, "first", torch.int32, device, (n,))
+    first_at = None if first is None else _numbers(first, "first", torch.int32, device, (n,))
     a = ibp_attn(TYPES[kind], kv_heads, kv_heads, dim, 1.0, 0)
-    check(lib().ibp_kv4_read(a, pages, lens_at, n, starts_at, first_at, rk, rv, _stream(stream, device)), "ibp_kv4_read")
+    status = _KV4_READ(a, pages, lens_at, n, starts_at, first_at, rk, rv, _stream(stream, device))
+    if status:
+        check(status, "ibp_kv4_read")
 
 
 def ibp_attn_decode4_workspace(n_seqs, q_heads, kv_heads, head_dim, max_len, weights):
@@ -182,26 +211,24 @@ def ibp_attn_decode4(q, keys, values, table, lens, max_len, out, lse=None, weigh
     device = _device(q, "q")
     if q.dtype not in TYPES:
         raise TypeError(f"q must be bfloat16 or float16, not {q.dtype}")
-    rq = _rows(q, "q", q.dtype, device)
+    rq = _rows_of(q, "q", q.dtype, device)
     n, heads, dim = q.shape
     _tensor(keys, "keys", device)
     kv_heads = keys.shape[1] if keys.dim() == 4 else 0
     pages = _pool_of(keys, values, table, device, torch.uint8, 2, kv_heads, ibp_kv4_record(dim), "records")
     if table.shape[0] != n:
         raise ValueError("table must have a row for every sequence")
-    lens_at = _array(lens, "lens", torch.int32, device, (n,))
-    ro = _rows(out, "out", q.dtype, device, heads, dim)
-    lse_at = None if lse is None else _array(lse, "lse", torch.float32, device, (n, heads))
+    lens_at = _numbers(lens, "lens", torch.int32, device, (n,))
+    ro = _rows_of(out, "out", q.dtype, device, heads, dim)
+    lse_at = None if lse is None else _numbers(lse, "lse", torch.float32, device, (n, heads))
     weights_at, slots = None, 0
     if weights is not None:
-        weights_at = _array(weights, "weights", torch.float32, device)
-        if weights.dim() != 3 or weights.shape[:2] != (n, kv_heads):
-            raise ValueError("weights must be [sequences][kv_heads][slots]")
-        slots = weights.shape[2]
+        weights_at, slots = _tracked(weights, "weights", torch.float32, device, n, kv_heads, None)
     a = _attn(q, kv_heads, dim, scale)
     need = 0
     if workspace is None:
         need = ibp_attn_decode4_workspace(n, heads, kv_heads, dim, max_len, weights is not None)
     at, size, held = _space(workspace, need, device, stream)
-    check(lib().ibp_attn_decode4(a, rq, pages, lens_at, _count(max_len, "max_len"), ro, lse_at, weights_at, slots, at, size,
-                                 _stream(stream, device)), "ibp_attn_decode4")
+    status = _DECODE4(a, rq, pages, lens_at, _count(max_len, "max_len"), ro, lse_at, weights_at, slots, at, size, _stream(stream, device))
+    if status:
+        check(status, "ibp_attn_decode4")
