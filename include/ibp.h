@@ -536,7 +536,7 @@ ibp_status ibp_kv_evict(const ibp_attn *a, const ibp_pages *pages, const int32_t
  * A record is what a 4-bit cache holds of one token's key or value of one head, ibp_kv4_record(head_dim)
  * bytes in groups of 32 values (the last group of a head may be shorter), G of them: 16 G bytes of
  * codes (byte i of a group has value 2 i in its low half and 2 i + 1 in its high half), G steps, G
- * centres, both of the cache's type, then padding to 16 bytes that is neither read nor written. A value is
+ * centres, both of the cache's type, then padding to 16 bytes whose content is of no matter and stays. A value is
  *   centre + (code - 7.5) step
  * of its group. ibp_pages describes pools of records as well: a row is a record, strides count 2 bytes as
  * ever (multiples of 8). So ibp_kv_evict takes them as rows of record / 2 16-bit values (that as its head_dim), and

@@ -52,7 +52,7 @@ struct Place {
     uint32_t row;
 };
 __device__ __forceinline__ bool find_slot(const Pages &pg, uint32_t seq, int64_t slot, Place &p) {
-    if (slot < 0 || slot >= (int64_t)pg.table_stride * pg.page_tokens || slot >= 0x7fffffff) return false;
+    if (pg.n_pages == 0 || slot < 0 || slot >= (int64_t)pg.table_stride * pg.page_tokens || slot >= 0x7fffffff) return false;
     const uint32_t s = (uint32_t)slot, i = pg.page_magic ? __umulhi(s, pg.page_magic) >> pg.page_shift : s >> pg.page_shift;
     const int32_t page = pg.table[(int64_t)seq * pg.table_stride + i];
     p.page = page;
@@ -68,9 +68,19 @@ template <class T>
 __device__ __forceinline__ f32x4 widen(u32x2 x) {
     return f32x4{T::value((uint16_t)x[0]), T::value((uint16_t)(x[0] >> 16)), T::value((uint16_t)x[1]), T::value((uint16_t)(x[1] >> 16))};
 }
+// A number that is rounded to 32 bits before it is to 16: the instructions that do both at once for float16 round once.
+template <class T>
+__device__ __forceinline__ float rounded(float x) {
+    if constexpr (T::kExp == F16::kExp) asm("" : "+v"(x));
+    return x;
+}
+template <class T>
+__device__ __forceinline__ uint32_t narrow(float x, float y) {
+    return T::pack(rounded<T>(x), rounded<T>(y));
+}
 template <class T>
 __device__ __forceinline__ u32x2 narrow(f32x4 x) {
-    return u32x2{T::pack(x[0], x[1]), T::pack(x[2], x[3])};
+    return u32x2{narrow<T>(x[0], x[1]), narrow<T>(x[2], x[3])};
 }
 
 // x a + y b, each product and the sum rounded.
@@ -118,9 +128,9 @@ __device__ __forceinline__ uint32_t codes_of(const float *x, uint32_t there, uin
         hi = fmaxf(hi, __shfl_xor(hi, d));
         bad |= __shfl_xor((int)bad, d) != 0;
     }
-    centre16 = (uint16_t)T::pack(lo * 0.5f + hi * 0.5f, 0.f);
+    centre16 = (uint16_t)narrow<T>(lo * 0.5f + hi * 0.5f, 0.f);
     const float centre = T::value(centre16);
-    step16 = (uint16_t)T::pack(fmaxf(hi - centre, centre - lo) * (2.f / 15.f), 0.f);
+    step16 = (uint16_t)narrow<T>(fmaxf(hi - centre, centre - lo) * (2.f / 15.f), 0.f);
     const float step = T::value(step16);
     if (bad || !(fabsf(centre) < __builtin_inff()) || !(step < __builtin_inff())) {
         centre16 = step16 = (uint16_t)(T::kExp | (T::kExp >> 1 & ~T::kExp));      // (quiet NaN)
@@ -345,7 +355,7 @@ __global__ __launch_bounds__(kThreads) void k_kv4_read(Read4 a, uint32_t octs_lo
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf((float)(code[n] >> 4 * i & 15) - 7.5f, s, c);
         put<N>((uint8_t *)out.data + ((int64_t)row * out.row + (int64_t)(is_k ? h : h - a.kv_heads) * out.head + d) * 2,
-               Frag{T::pack(x[0], x[1]), T::pack(x[2], x[3]), T::pack(x[4], x[5]), T::pack(x[6], x[7])});
+               Frag{narrow<T>(x[0], x[1]), narrow<T>(x[2], x[3]), narrow<T>(x[4], x[5]), narrow<T>(x[6], x[7])});
     }
 }
 

@@ -103,6 +103,19 @@ def test_read(ibp, kind, dim, page):
         assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("kind,kv_heads,dim", [(BF16, 8, 128), (F16, 17, 40), (BF16, 3, 256)])
+def test_read_many_rows(ibp, kind, kv_heads, dim):
+    c = Cache(kind, kv_heads, dim, [1500, 0, 700], 24, seed=dim)
+    k, v = (torch.full((2201, kv_heads, dim), 7.0, dtype=kind, device="cuda") for _ in range(2))
+    ibp.ibp_kv4_read(c.keys.cuda(), c.values.cuda(), c.table.cuda(), int32(c.lens), k, v, int32([0, 1500, 1500, 2200]))
+    for pool, got in ((c.keys, k.cpu()), (c.values, v.cpu())):
+        want = torch.full_like(got, 7.0)
+        for b, first, n in ((0, 0, 1500), (2, 1500, 700)):
+            for h in range(kv_heads):
+                want[first:first + n, h] = values_of(c.rows(pool, b, h, range(n)), dim, kind, torch.float32).to(kind)
+        assert torch.equal(got, want)
+
+
 def test_read_from_a_slot_on(ibp):
     """`first`, fewer rows than slots, absent pages, a row per sequence, and numbers outside everything."""
     c = Cache(BF16, 2, 64, [50, 64, 30], 16, seed=2)
@@ -245,6 +258,34 @@ def test_decode_offsets_past_32_bits(ibp):
     v.copy_(c.values.cuda())
     out, lse, _ = decode(ibp, c, q, keys=k, values=v)
     assert torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+def test_decode_as_many_slots_as_there_can_be(ibp):
+    """2^31 - 256 slots, the most that a call takes, all of them one record (strides of 0): lse = x + ln n and the output is what the
+    record stands for; a split left out would show as ln of what is left of n, 2e-3 less."""
+    n, page = (1 << 31) - 256, 1 << 24
+    g = torch.Generator().manual_seed(1)
+    q = torch.randn(1, 1, 32, generator=g).to(BF16)
+    record = records_of(torch.randn(2, 32, generator=g).to(BF16).float(), BF16)
+    pools = [x.view(1, 1, 1, 32).cuda().expand(1, 1, page, 32) for x in record]
+    table = torch.zeros(1, 128, dtype=torch.int32, device="cuda")
+    out, lse = torch.zeros(1, 1, 32, dtype=BF16, device="cuda"), torch.zeros(1, 1, device="cuda")
+    ibp.ibp_attn_decode4(q.cuda(), *pools, table, int32([n]), n, out, lse)
+    x = (q[0, 0].double() @ values_of(record[0], 32, BF16)).item() * 32 ** -0.5
+    want = x + torch.log(torch.tensor(float(n), dtype=torch.float64)).item()
+    assert abs(lse.item() - want) <= 2.0 ** -19 * (abs(want) + abs(x))
+    code, step, centre = parts_of(record[1], 32, BF16)
+    value = code * step + centre
+    # (the output's rounding, and 2^16 sums that each wave adds up for its 2^20 slots, each off by up to u32 of 55 step + |centre|)
+    assert ((out[0, 0].cpu().double() - value).abs() <= 2.0 ** -8 * 1.01 * value.abs() + 2.0 ** 16 * U32 * (55 * step + centre.abs())).all()
+
+
+def test_decode_of_many_heads_under_a_wide_bound(ibp):
+    """max_len is only a bound: with as large a one as there is, a short cache is read as it is."""
+    c = Cache(BF16, 64, 64, [100], 128, seed=17)
+    q = queries(c, 64)
+    out, lse, _ = decode(ibp, c, q, table=torch.cat([c.table, torch.zeros(1, (1 << 24) - 1, dtype=torch.int32)], 1), max_len=(1 << 31) - 256)
+    check(c, q, out, lse)
 
 
 @pytest.mark.parametrize("kind", [F16, BF16])

@@ -204,6 +204,38 @@ def test_an_empty_pool_takes_nothing(ibp, four):
 
 
 @FOUR
+def test_an_empty_pool_without_a_table(ibp, four):
+    """Nothing is looked up: a null table is allowed where there are no pages."""
+    from paper_2605_30728_amd import attention as at
+    c = Case(BF16, 4, 2, 64, 64, True, [4], [0])
+    k, v, q, out, rotation, lens, starts = c.k.cuda(), c.v.cuda(), c.q.cuda(), c.q.cuda(), c.rotation.cuda(), int32(c.lens), starts_of(c.new)
+    rows = lambda x: at.ibp_rows(x.data_ptr(), x.shape[0], x.stride(0), x.stride(1))  # noqa: E731
+    from paper_2605_30728_amd.kv_cache import ibp_rotation
+    pages = at.ibp_pages(None, None, 0, 16, 3, None, *[0] * 6)
+    status = getattr(ibp.lib(), "ibp_kv4_append" if four else "ibp_kv_append")(
+        at.ibp_attn(0, 4, 2, 64, 1.0, 0), rows(k), rows(v), rows(q), rows(out), ibp_rotation(rotation.data_ptr(), rotation.shape[0], 64, 1),
+        starts.data_ptr(), 1, pages, lens.data_ptr(), lens.data_ptr(), None, None, 0, torch.cuda.current_stream().cuda_stream)
+    assert status == ibp.IBP_OK
+    torch.cuda.synchronize()
+    for row, _, _, position in c.places():
+        near(out[row].cpu(), c.q[row], c.rotation[position], c)
+    if four:
+        assert ibp.lib().ibp_kv4_read(at.ibp_attn(0, 2, 2, 64, 1.0, 0), pages, lens.data_ptr(), 1, starts.data_ptr(), None, rows(k), rows(v),
+                                      torch.cuda.current_stream().cuda_stream) == ibp.IBP_OK
+        torch.cuda.synchronize()
+        assert torch.equal(k.cpu(), c.k) and torch.equal(v.cpu(), c.v)
+
+
+@FOUR
+@pytest.mark.parametrize("kind,heads,kv_heads,dim,turned,halves", [(BF16, 32, 8, 128, 128, True), (F16, 28, 4, 80, 48, True),
+                                                                   (BF16, 17, 17, 40, 40, False), (F16, 6, 3, 256, 256, True)])
+def test_calls_of_many_rows(ibp, four, kind, heads, kv_heads, dim, turned, halves):
+    """Several items of every lane on their way; heads that do not fill the last part of a row."""
+    c = Case(kind, heads, kv_heads, dim, turned, halves, [700, 0, 3, 1500], [1, 5, 20, 0], page=24, gone=7, after=1, seed=heads)
+    check(c, four, *append(ibp, c, four))
+
+
+@FOUR
 def test_layouts(ibp, four):
     """Rows as views of one projection, pools in [page][token][head] order, keys and values interleaved."""
     c = Case(BF16, 6, 2, 64, 64, True, [9, 30], [2, 0], seed=5)
