@@ -10,10 +10,14 @@ every conversation is held at a budget of slots.
                (row ids in the order of the pages), and once more packed for the prompts
   2. prompt    ibp_attn_prompt: the new turn's rows against history and turn, all sequences at once
   3. weights   ibp_attn_key_weights: what every key received from the turn
-  4. evict     ibp_kv_evict: the most recent and the heaviest slots stay
-  5. tokens    ibp_attn_decode over the pages, which goes on adding up weights, then ibp_kv_evict in place
+  4. append    ibp_kv_append: the turn's keys and values join the history in the pages
+  5. evict     ibp_kv_evict: the most recent and the heaviest slots stay
+  6. tokens    ibp_kv_append, ibp_attn_decode over the pages, which goes on adding up weights, then
+               ibp_kv_evict in place
 
-Queries, keys and values are random here; in a model they are the layer's projections.
+Queries, keys and values are random here; in a model they are the layer's projections, and ibp_kv_append turns them by
+their positions on the way. With pools of ibp_kv4_record(dim) bytes a token, ibp_kv4_append, ibp_attn_decode4 and
+ibp_kv4_read hold such a cache in 4 bits.
 """
 import os
 import sys
@@ -52,15 +56,15 @@ class Cache:
         self.lens = torch.zeros(seqs, dtype=torch.int32, device=device)
         self.next = torch.zeros(seqs, dtype=torch.int32, device=device)
 
-    def append(self, seq, k, v):
-        """One token for each of the sequences `seq` (their numbers): k, v [n][kv_heads][dim]."""
-        at = self.lens[seq].long()
-        page, row = self.table[seq, at // self.page].long(), at % self.page
-        self.k[page, :, row], self.v[page, :, row] = k, v
-        self.weights[seq, :, at] = 0
-        self.positions[seq, :, at] = self.next[seq, None]
-        self.lens[seq] += 1
-        self.next[seq] += 1
+    def append(self, k, v, n=None):
+        """The packed rows k, v [rows][kv_heads][dim], n (their numbers) of each sequence; None: one token of each."""
+        starts = None
+        if n is not None:
+            starts = torch.tensor(np.concatenate(([0], np.cumsum(n))), dtype=torch.int32, device=self.k.device)
+        more = 1 if n is None else starts.diff()
+        self.lens += more
+        self.next += more
+        ibp.ibp_kv_append(k, v, self.k, self.v, self.table, self.lens, self.next, starts, weights=self.weights, positions=self.positions)
 
     def evict(self, budget, recent, longest):
         ibp.ibp_kv_evict(self.k, self.v, self.table, self.lens, longest, budget, recent, self.next, self.weights,
@@ -97,7 +101,10 @@ def run(history=(700, 0, 1333), turn=(90, 33, 257), tokens=8, q_heads=32, kv_hea
             ibp.ibp_gather_decompress_device(handle, ids.reshape(-1).contiguous(), pool[first:first + whole // page])
             ids = (x * kv_heads + heads[None, :]) * total + token[:h, None]                        # [token][head]
             ibp.ibp_gather_decompress_device(handle, ids.reshape(-1).contiguous(), packed[x, k_starts[b]:k_starts[b] + h])
+        cache.positions[b, :, :h] = torch.arange(h, device=device, dtype=torch.int32)
         start += h
+    cache.lens += torch.tensor(history, dtype=torch.int32, device=device)
+    cache.next += cache.lens
 
     # 2. and 3. the new turn
     q = random(int(q_starts[-1]), q_heads, dim)
@@ -107,27 +114,25 @@ def run(history=(700, 0, 1333), turn=(90, 33, 257), tokens=8, q_heads=32, kv_hea
     weights = torch.zeros(kv_heads, packed.shape[1], device=device)
     ibp.ibp_attn_prompt(q, packed[0], packed[1], *starts, out, lse)
     ibp.ibp_attn_key_weights(q, packed[0], *starts, lse, weights)
-    for b, (h, t) in enumerate(zip(history, turn)):
-        n, at = h + t, int(k_starts[b])
-        slot = torch.arange(h, n, device=device)
-        where = cache.table[b, slot // page].long(), slice(None), slot % page
-        cache.k[where], cache.v[where] = new[0, at + h:at + n], new[1, at + h:at + n]
-        cache.weights[b, :, :n] = weights[:, at:at + n]
-        cache.positions[b, :, :n] = torch.arange(n, device=device, dtype=torch.int32)
-        cache.lens[b] = cache.next[b] = n
-    prompt = dict(q=q, k=packed[0], v=packed[1], q_starts=q_starts, k_starts=k_starts, out=out, lse=lse, weights=weights)
 
     # 4.
-    cache.evict(budget, recent, longest)
+    kept = [torch.arange(int(k_starts[b]) + h, int(k_starts[b + 1]), device=device) for b, h in enumerate(history)]
+    cache.append(*new[:, torch.cat(kept)], turn)
+    for b, (h, t) in enumerate(zip(history, turn)):
+        n, at = h + t, int(k_starts[b])
+        cache.weights[b, :, :n] = weights[:, at:at + n]
+    prompt = dict(q=q, k=packed[0], v=packed[1], q_starts=q_starts, k_starts=k_starts, out=out, lse=lse, weights=weights)
 
     # 5.
-    everyone = torch.arange(seqs, device=device)
+    cache.evict(budget, recent, longest)
+
+    # 6.
     held = min(longest, budget) + 1
     token_out = torch.empty(seqs, q_heads, dim, dtype=torch.bfloat16, device=device)
     workspace = torch.empty(max(ibp.ibp_attn_decode_workspace(seqs, q_heads, kv_heads, dim, cache.slots, True), 1),
                             dtype=torch.uint8, device=device)
     for _ in range(tokens):
-        cache.append(everyone, random(seqs, kv_heads, dim), random(seqs, kv_heads, dim))
+        cache.append(random(seqs, kv_heads, dim), random(seqs, kv_heads, dim))
         q1 = random(seqs, q_heads, dim)
         before = cache.weights.clone() if on_token else None
         ibp.ibp_attn_decode(q1, cache.k, cache.v, cache.table, cache.lens, held, token_out, weights=cache.weights,
