@@ -172,15 +172,16 @@ __device__ __forceinline__ bool find_where(const Append &a, uint32_t row, Where 
     return true;
 }
 
-// Items, of eight values each, that a lane has on their way together: four fill the chip's memory system, and in calls of too few
-// rows for that one each is sooner done.
-constexpr int kMany = 4;
-constexpr uint64_t kFewWaves = 2048;     // (of four items)
+// Items, of eight values each, that a lane has on their way together: four fill the chip's memory system (8,192 rows appended 47 us,
+// with two and eight 50 and 51); those that are held in 4 bits, with more to do for each, two (51 us with four or one, 47). In
+// calls of too few rows for that one each is sooner done (64 rows 3.8 us instead of 5.5).
+constexpr int kMany = 4, kManyFour = 2;
+constexpr uint64_t kFewWaves = 2048;     // (of so many items)
 
-// Waves are shared out as `parts` per row: each takes 64 N items of its heads, first of those that stay 16 bits wide (`wide`
-// parts: queries, and without FOUR keys and values), then of those that are held in 4. A lane's items are the same eight
+// Waves are shared out as `parts` per row: each takes 64 N items of its heads that stay 16 bits wide (the first
+// `wide` parts: queries, and without FOUR keys and values), or 64 M of those that are held in 4. A lane's items are the same eight
 // values of several heads, `octs` (a power of two, at least the head's) lanes per head, so that it needs the angles once.
-template <class T, bool FOUR, int N>
+template <class T, bool FOUR, int N, int M>
 __global__ __launch_bounds__(kThreads) void k_kv_append(Append a, uint32_t wide_log2, uint32_t four_log2, uint32_t wide, uint32_t parts) {
     const uint32_t wave = (uint32_t)uniform((int)(blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6)));
     const uint32_t row = wave / parts, part = wave - row * parts, lane = threadIdx.x & 63;
@@ -237,7 +238,7 @@ __global__ __launch_bounds__(kThreads) void k_kv_append(Append a, uint32_t wide_
         }
     } else if constexpr (FOUR) {
         const uint32_t groups = record_groups(a.dim), oct = lane & ((1u << four_log2) - 1), d = oct * 8;
-        const uint32_t head0 = (((part - wide) * N * 64) + lane) >> four_log2, head_step = 64u >> four_log2;
+        const uint32_t head0 = (((part - wide) * M * 64) + lane) >> four_log2, head_step = 64u >> four_log2;
         const uint32_t have = min(max((int)a.dim - (int)d, 0), 8);
         const bool turn = d < a.turned;
         // of pairs that are apart the other quads
@@ -248,7 +249,7 @@ __global__ __launch_bounds__(kThreads) void k_kv_append(Append a, uint32_t wide_
             other[i] = at < half ? at + half : at - half;
             pair[i] = at < half ? at : at - half;
         }
-        u32x2 x[N][2], y[N][2];
+        u32x2 x[M][2], y[M][2];
         auto in_heads = [&](int n, uint32_t &head, bool &is_k) {
             const uint32_t h = head0 + n * head_step;
             is_k = h < a.kv_heads;
@@ -256,7 +257,7 @@ __global__ __launch_bounds__(kThreads) void k_kv_append(Append a, uint32_t wide_
             return h < 2 * a.kv_heads && oct < groups * 4;
         };
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
+        for (int n = 0; n < M; ++n) {
             uint32_t head;
             bool is_k;
             if (!in_heads(n, head, is_k) || !have) continue;
@@ -280,7 +281,7 @@ __global__ __launch_bounds__(kThreads) void k_kv_append(Append a, uint32_t wide_
             }
         }
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
+        for (int n = 0; n < M; ++n) {
             uint32_t head;
             bool is_k;
             if (!in_heads(n, head, is_k)) continue;
@@ -380,18 +381,18 @@ hipError_t launch_append(const Append &a, hipStream_t stream) {
     if (a.rows == 0 || a.n_seqs == 0) return hipSuccess;
     const uint32_t wide_log2 = log2_up(a.dim / 8), four_log2 = log2_up(record_groups(a.dim) * 4);
     const uint64_t wide_heads = a.q_heads + (a.four ? 0ull : 2ull * a.kv_heads), four_heads = a.four ? 2ull * a.kv_heads : 0;
-    auto launch = [&](auto kernel, int items) {
-        const uint64_t wide = parts_of(wide_heads, wide_log2, items), parts = wide + parts_of(four_heads, four_log2, items);
+    auto launch = [&](auto kernel, int items, int items_four) {
+        const uint64_t wide = parts_of(wide_heads, wide_log2, items), parts = wide + parts_of(four_heads, four_log2, items_four);
         const uint32_t blocks = blocks_of(a.rows, parts);
         if (!blocks) return hipErrorInvalidConfiguration;
         kernel<<<dim3(blocks), dim3(kThreads), 0, stream>>>(a, wide_log2, four_log2, (uint32_t)wide, (uint32_t)parts);
         return hipGetLastError();
     };
-    const bool many = a.rows * (parts_of(wide_heads, wide_log2, kMany) + parts_of(four_heads, four_log2, kMany)) >= kFewWaves;
+    const bool many = a.rows * (parts_of(wide_heads, wide_log2, kMany) + parts_of(four_heads, four_log2, kManyFour)) >= kFewWaves;
     auto of_type = [&](auto type) {
         using T = decltype(type);
-        if (many) return launch(a.four ? k_kv_append<T, true, kMany> : k_kv_append<T, false, kMany>, kMany);
-        return launch(a.four ? k_kv_append<T, true, 1> : k_kv_append<T, false, 1>, 1);
+        if (many) return launch(a.four ? k_kv_append<T, true, kMany, kManyFour> : k_kv_append<T, false, kMany, kManyFour>, kMany, kManyFour);
+        return launch(a.four ? k_kv_append<T, true, 1, 1> : k_kv_append<T, false, 1, 1>, 1, 1);
     };
     return a.f16 ? of_type(F16{}) : of_type(Bf16{});
 }
