@@ -66,8 +66,21 @@ __device__ __forceinline__ bool find_slot(const Pages &pg, uint32_t seq, int64_t
     return (uint32_t)page < pg.n_pages;
 }
 
-__device__ __forceinline__ uint8_t *at_slot(const Pool &p, const Place &x, uint32_t head) {
-    return (uint8_t *)p.data + (x.page * p.page + (int64_t)head * p.head + (int64_t)x.row * p.token) * 2;
+// Where the first head's row is, the same for a whole wave, and how far apart the heads are, in bytes: what a lane's own head needs beside
+// is one product.
+struct Heads {
+    uint8_t *first;
+    int64_t step;
+};
+__device__ __forceinline__ Heads heads_at(const Pool &p, const Place &x) {
+    return Heads{(uint8_t *)p.data + (x.page * p.page + (int64_t)x.row * p.token) * 2, p.head * 2};
+}
+__device__ __forceinline__ Heads heads_at(const Rows &r, uint32_t row) {
+    return Heads{(uint8_t *)r.data + (int64_t)row * r.row * 2, r.head * 2};
+}
+__device__ __forceinline__ uint8_t *head_of(const Heads &h, uint32_t head) { return h.first + (int64_t)head * h.step; }
+__device__ __forceinline__ Heads either(bool first, const Heads &a, const Heads &b) {
+    return Heads{first ? a.first : b.first, first ? a.step : b.step};
 }
 
 template <class T>
@@ -200,6 +213,7 @@ __global__ __launch_bounds__(kThreads) void k_kv_append(Append a, uint32_t wide_
         // both quads of four pairs, so that nothing that another lane writes is read: queries may be turned in place
         const bool turn = d < a.turned, apart = turn && a.halves;
         const uint32_t q0 = apart ? oct * 4 : d, q1 = apart ? half + oct * 4 : d + 4;
+        const Heads in_q = heads_at(a.q, row), in_k = heads_at(a.k, row), in_v = heads_at(a.v, row);
         u32x2 x[N], y[N];
         auto in_heads = [&](int n, uint32_t &head, uint32_t &which) {
             const uint32_t h = head0 + n * head_step;
@@ -211,13 +225,13 @@ __global__ __launch_bounds__(kThreads) void k_kv_append(Append a, uint32_t wide_
         for (int n = 0; n < N; ++n) {
             uint32_t head, which;
             if (!in_heads(n, head, which)) continue;
-            const Rows &in = which == 0 ? a.q : which == 1 ? a.k : a.v;
             const bool mixed = which != 2;
-            const uint8_t *from = (const uint8_t *)in.data + ((int64_t)row * in.row + (int64_t)head * in.head) * 2;
+            const uint8_t *from = head_of(either(which == 0, in_q, either(which == 1, in_k, in_v)), head);
             x[n] = *reinterpret_cast<const u32x2 *>(from + (mixed ? q0 : d) * 2);
             y[n] = *reinterpret_cast<const u32x2 *>(from + (mixed ? q1 : d + 4) * 2);
         }
         if (!find_where(a, row, w)) return;
+        const Heads out_q = heads_at(a.q_out, row), out_k = heads_at(a.pg.k, w.place), out_v = heads_at(a.pg.v, w.place);
         Angles at{};
         if (turn) at = angles_at(w.angles + oct * 8);
 #pragma unroll
@@ -225,8 +239,7 @@ __global__ __launch_bounds__(kThreads) void k_kv_append(Append a, uint32_t wide_
             uint32_t head, which;
             if (!in_heads(n, head, which) || (which != 0 && !w.there)) continue;
             const bool mixed = which != 2;
-            uint8_t *to = which == 0 ? (uint8_t *)a.q_out.data + ((int64_t)row * a.q_out.row + (int64_t)head * a.q_out.head) * 2
-                                     : at_slot(which == 1 ? a.pg.k : a.pg.v, w.place, head);
+            uint8_t *to = head_of(either(which == 0, out_q, either(which == 1, out_k, out_v)), head);
             if (mixed && turn) {
                 f32x4 u = widen<T>(x[n]), v = widen<T>(y[n]);
                 if (a.halves) {
@@ -255,6 +268,7 @@ __global__ __launch_bounds__(kThreads) void k_kv_append(Append a, uint32_t wide_
             other[i] = at < half ? at + half : at - half;
             pair[i] = at < half ? at : at - half;
         }
+        const Heads in_k = heads_at(a.k, row), in_v = heads_at(a.v, row);
         u32x2 x[M][2], y[M][2];
         auto in_heads = [&](int n, uint32_t &head, bool &is_k) {
             const uint32_t h = head0 + n * head_step;
@@ -267,8 +281,7 @@ __global__ __launch_bounds__(kThreads) void k_kv_append(Append a, uint32_t wide_
             uint32_t head;
             bool is_k;
             if (!in_heads(n, head, is_k) || !have) continue;
-            const Rows &in = is_k ? a.k : a.v;
-            const uint8_t *from = (const uint8_t *)in.data + ((int64_t)row * in.row + (int64_t)head * in.head) * 2;
+            const uint8_t *from = head_of(either(is_k, in_k, in_v), head);
 #pragma unroll
             for (int i = 0; i < 2; ++i) x[n][i] = *reinterpret_cast<const u32x2 *>(from + (d + 4 * i) * 2);
             if (is_k && turn && a.halves) {
@@ -277,6 +290,7 @@ __global__ __launch_bounds__(kThreads) void k_kv_append(Append a, uint32_t wide_
             }
         }
         if (!find_where(a, row, w) || !w.there) return;
+        const Heads out_k = heads_at(a.pg.k, w.place), out_v = heads_at(a.pg.v, w.place);
         Angles at[2]{};
         if (turn) {
             if (a.halves) {
@@ -308,7 +322,7 @@ __global__ __launch_bounds__(kThreads) void k_kv_append(Append a, uint32_t wide_
             const float z[8] = {u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
             uint16_t step, centre;
             const uint32_t code = codes_of<T>(z, have, step, centre);
-            uint8_t *to = at_slot(is_k ? a.pg.k : a.pg.v, w.place, head);
+            uint8_t *to = head_of(either(is_k, out_k, out_v), head);
             *reinterpret_cast<uint32_t *>(to + oct * 4) = code;
             if ((oct & 3) == 0) {
                 uint8_t *meta = to + groups * kGroupBytes + oct / 4 * 2;
@@ -340,13 +354,14 @@ __global__ __launch_bounds__(kThreads) void k_kv4_read(Read4 a, uint32_t octs_lo
     const uint32_t groups = record_groups(a.dim), oct = lane & ((1u << octs_log2) - 1), d = oct * 8;
     const uint32_t head0 = ((part * N * 64) + lane) >> octs_log2, head_step = 64u >> octs_log2;
     if (d >= a.dim) return;
+    const Heads in_k = heads_at(a.pg.k, place), in_v = heads_at(a.pg.v, place), out_k = heads_at(a.k, row), out_v = heads_at(a.v, row);
     uint32_t code[N];
     uint16_t step[N], centre[N];
 #pragma unroll
     for (int n = 0; n < N; ++n) {
         const uint32_t h = min(head0 + n * head_step, 2 * a.kv_heads - 1);
         const bool is_k = h < a.kv_heads;
-        const uint8_t *from = at_slot(is_k ? a.pg.k : a.pg.v, place, is_k ? h : h - a.kv_heads), *meta = from + groups * kGroupBytes + oct / 4 * 2;
+        const uint8_t *from = head_of(either(is_k, in_k, in_v), is_k ? h : h - a.kv_heads), *meta = from + groups * kGroupBytes + oct / 4 * 2;
         code[n] = *reinterpret_cast<const uint32_t *>(from + oct * 4);
         step[n] = *reinterpret_cast<const uint16_t *>(meta);
         centre[n] = *reinterpret_cast<const uint16_t *>(meta + groups * 2);
@@ -356,12 +371,11 @@ __global__ __launch_bounds__(kThreads) void k_kv4_read(Read4 a, uint32_t octs_lo
         const uint32_t h = head0 + n * head_step;
         if (h >= 2 * a.kv_heads) return;
         const bool is_k = h < a.kv_heads;
-        const Rows &out = is_k ? a.k : a.v;
         const float s = T::value(step[n]), c = T::value(centre[n]);
         float x[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf((float)(code[n] >> 4 * i & 15) - 7.5f, s, c);
-        put<N>((uint8_t *)out.data + ((int64_t)row * out.row + (int64_t)(is_k ? h : h - a.kv_heads) * out.head + d) * 2,
+        put<N>(head_of(either(is_k, out_k, out_v), is_k ? h : h - a.kv_heads) + d * 2,
                Frag{narrow<T>(x[0], x[1]), narrow<T>(x[2], x[3]), narrow<T>(x[4], x[5]), narrow<T>(x[6], x[7])});
     }
 }
