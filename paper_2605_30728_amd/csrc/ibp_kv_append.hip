@@ -6,11 +6,11 @@
 //   per 32 values  centre = type((lo + hi) / 2),  step = type(2/15 max(hi - centre, centre - lo)),
 //   code = round((x - centre) / step + 7.5) clamped to 0 .. 15,  value = centre + (code - 7.5) step.
 //
-// Large calls are bound by HBM, into records by the conversions beside it: 8,192 rows of 32/8 heads of 128 in
-// bfloat16 47 us into 16-bit pages (206 MB, 4.4 TB/s; a large copy 5.2) and 47 into records (186 MB, 3.9 TB/s, the vector unit
-// busy half of the time), 32,768 slots of 8 heads of 128 read back 29 us (176 MB, 6.0 TB/s: 134 of them written
-// around the caches). Small ones by the look-ups, each of which waits for the one before (the row's sequence, its length, its
-// page): one row 3.1 us, 64 rows 3.8, into records 5.0, of which a launch is about 2.
+// Large calls are bound by HBM: 8,192 rows of 32/8 heads of 128 in bfloat16 39 us into 16-bit pages (206 MB, 5.3 TB/s, as a large
+// copy) and 45 into records (182 MB, 4.0 TB/s, with the conversions between the loads and the stores), 32,768 slots of 8 heads of
+// 128 read back 29 us (176 MB, 6.1 TB/s: 134 of them written around the caches). Small ones by the look-ups, each of
+// which waits for the one before (the row's sequence, its length, its page): one row 2.8 us, 64 rows 3.5, into records 4.6,
+// of which a launch is about 2.
 #include "ibp_attn_wave.hpp"
 #include "ibp_kv_cache.hpp"
 
@@ -129,6 +129,12 @@ __device__ __forceinline__ void turn_neighbours(f32x4 &u, f32x4 &v, const Angles
     v = f32x4{p[2], q[2], p[3], q[3]};
 }
 
+// x of lane ^ D, of the four that a lane is one of.
+template <int D>
+__device__ __forceinline__ float beside(float x) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(x), D == 1 ? 0xb1 : 0x4e, 0xf, 0xf, true));
+}
+
 // Eight values of a head, in the lanes of its group of 32 (four in a row), as their dword of codes; step and centre.
 template <class T>
 __device__ __forceinline__ uint32_t codes_of(const float *x, uint32_t there, uint16_t &step16, uint16_t &centre16) {
@@ -141,12 +147,11 @@ __device__ __forceinline__ uint32_t codes_of(const float *x, uint32_t there, uin
             hi = fmaxf(hi, x[i]);
             bad |= !(fabsf(x[i]) < __builtin_inff());
         }
-#pragma unroll
-    for (int d = 1; d < 4; d <<= 1) {
-        lo = fminf(lo, __shfl_xor(lo, d));
-        hi = fmaxf(hi, __shfl_xor(hi, d));
-        bad |= __shfl_xor((int)bad, d) != 0;
-    }
+    lo = fminf(lo, beside<1>(lo));
+    hi = fmaxf(hi, beside<1>(hi));
+    lo = fminf(lo, beside<2>(lo));
+    hi = fmaxf(hi, beside<2>(hi));
+    bad = (__ballot(bad) >> (threadIdx.x & 60) & 15) != 0;
     centre16 = (uint16_t)narrow<T>(lo * 0.5f + hi * 0.5f, 0.f);
     const float centre = T::value(centre16);
     step16 = (uint16_t)narrow<T>(fmaxf(hi - centre, centre - lo) * (2.f / 15.f), 0.f);
@@ -166,7 +171,7 @@ __device__ __forceinline__ uint32_t codes_of(const float *x, uint32_t there, uin
 }
 
 // A store of a large call (N items a lane): around the caches, which its rows would leave unread (32,768 slots read back 29 us instead
-// of 38, 8,192 rows appended 47 instead of 49). What a small call writes is read next, and stays.
+// of 38, 8,192 rows appended 47 instead of 49 when that was chosen). What a small call writes is read next, and stays.
 template <int N, class X>
 __device__ __forceinline__ void put(uint8_t *to, X x) {
     if constexpr (N == 1) *reinterpret_cast<X *>(to) = x;
@@ -191,16 +196,16 @@ __device__ __forceinline__ bool find_where(const Append &a, uint32_t row, Where 
     return true;
 }
 
-// Items, of eight values each, that a lane has on their way together: four fill the chip's memory system (8,192 rows appended 47 us,
-// with two and eight 50 and 51); those that are held in 4 bits, with more to do for each, two (51 us with four or one, 47). In
-// calls of too few rows for that one each is sooner done (64 rows 3.8 us instead of 5.5).
-constexpr int kMany = 4, kManyFour = 2;
+// Items, of eight values each, that a lane has on their way together: four fill the chip's memory system (8,192 rows appended 39 us,
+// with two 41.5, with eight 40; into records 45, with two 53). In calls of too few rows for that one each is sooner done
+// (64 rows 3.5 us instead of 5.5).
+constexpr int kMany = 4;
 constexpr uint64_t kFewWaves = 2048;     // (of so many items)
 
-// Waves are shared out as `parts` per row: each takes 64 N items of its heads that stay 16 bits wide (the first
-// `wide` parts: queries, and without FOUR keys and values), or 64 M of those that are held in 4. A lane's items are the same eight
+// Waves are shared out as `parts` per row: each takes 64 N items of its heads, first of those that stay 16 bits wide (`wide`
+// parts: queries, and without FOUR keys and values), then of those that are held in 4. A lane's items are the same eight
 // values of several heads, `octs` (a power of two, at least the head's) lanes per head, so that it needs the angles once.
-template <class T, bool FOUR, int N, int M>
+template <class T, bool FOUR, int N>
 __global__ __launch_bounds__(kThreads) void k_kv_append(Append a, uint32_t wide_log2, uint32_t four_log2, uint32_t wide, uint32_t parts) {
     const uint32_t wave = (uint32_t)uniform((int)(blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6)));
     const uint32_t row = wave / parts, part = wave - row * parts, lane = threadIdx.x & 63;
@@ -257,7 +262,7 @@ __global__ __launch_bounds__(kThreads) void k_kv_append(Append a, uint32_t wide_
         }
     } else if constexpr (FOUR) {
         const uint32_t groups = record_groups(a.dim), oct = lane & ((1u << four_log2) - 1), d = oct * 8;
-        const uint32_t head0 = (((part - wide) * M * 64) + lane) >> four_log2, head_step = 64u >> four_log2;
+        const uint32_t head0 = (((part - wide) * N * 64) + lane) >> four_log2, head_step = 64u >> four_log2;
         const uint32_t have = min(max((int)a.dim - (int)d, 0), 8);
         const bool turn = d < a.turned;
         // of pairs that are apart the other quads
@@ -269,7 +274,7 @@ __global__ __launch_bounds__(kThreads) void k_kv_append(Append a, uint32_t wide_
             pair[i] = at < half ? at : at - half;
         }
         const Heads in_k = heads_at(a.k, row), in_v = heads_at(a.v, row);
-        u32x2 x[M][2], y[M][2];
+        u32x2 x[N][2], y[N][2];
         auto in_heads = [&](int n, uint32_t &head, bool &is_k) {
             const uint32_t h = head0 + n * head_step;
             is_k = h < a.kv_heads;
@@ -277,7 +282,7 @@ __global__ __launch_bounds__(kThreads) void k_kv_append(Append a, uint32_t wide_
             return h < 2 * a.kv_heads && oct < groups * 4;
         };
 #pragma unroll
-        for (int n = 0; n < M; ++n) {
+        for (int n = 0; n < N; ++n) {
             uint32_t head;
             bool is_k;
             if (!in_heads(n, head, is_k) || !have) continue;
@@ -301,7 +306,7 @@ __global__ __launch_bounds__(kThreads) void k_kv_append(Append a, uint32_t wide_
             }
         }
 #pragma unroll
-        for (int n = 0; n < M; ++n) {
+        for (int n = 0; n < N; ++n) {
             uint32_t head;
             bool is_k;
             if (!in_heads(n, head, is_k)) continue;
@@ -401,18 +406,18 @@ hipError_t launch_append(const Append &a, hipStream_t stream) {
     if (a.rows == 0 || a.n_seqs == 0) return hipSuccess;
     const uint32_t wide_log2 = log2_up(a.dim / 8), four_log2 = log2_up(record_groups(a.dim) * 4);
     const uint64_t wide_heads = a.q_heads + (a.four ? 0ull : 2ull * a.kv_heads), four_heads = a.four ? 2ull * a.kv_heads : 0;
-    auto launch = [&](auto kernel, int items, int items_four) {
-        const uint64_t wide = parts_of(wide_heads, wide_log2, items), parts = wide + parts_of(four_heads, four_log2, items_four);
+    auto launch = [&](auto kernel, int items) {
+        const uint64_t wide = parts_of(wide_heads, wide_log2, items), parts = wide + parts_of(four_heads, four_log2, items);
         const uint32_t blocks = blocks_of(a.rows, parts);
         if (!blocks) return hipErrorInvalidConfiguration;
         kernel<<<dim3(blocks), dim3(kThreads), 0, stream>>>(a, wide_log2, four_log2, (uint32_t)wide, (uint32_t)parts);
         return hipGetLastError();
     };
-    const bool many = a.rows * (parts_of(wide_heads, wide_log2, kMany) + parts_of(four_heads, four_log2, kManyFour)) >= kFewWaves;
+    const bool many = a.rows * (parts_of(wide_heads, wide_log2, kMany) + parts_of(four_heads, four_log2, kMany)) >= kFewWaves;
     auto of_type = [&](auto type) {
         using T = decltype(type);
-        if (many) return launch(a.four ? k_kv_append<T, true, kMany, kManyFour> : k_kv_append<T, false, kMany, kManyFour>, kMany, kManyFour);
-        return launch(a.four ? k_kv_append<T, true, 1, 1> : k_kv_append<T, false, 1, 1>, 1, 1);
+        if (many) return launch(a.four ? k_kv_append<T, true, kMany> : k_kv_append<T, false, kMany>, kMany);
+        return launch(a.four ? k_kv_append<T, true, 1> : k_kv_append<T, false, 1>, 1);
     };
     return a.f16 ? of_type(F16{}) : of_type(Bf16{});
 }
