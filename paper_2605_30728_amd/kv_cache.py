@@ -258,7 +258,8 @@ def ibp_attn_decode4(q, keys, values, table, lens, max_len, out, lse=None, weigh
     weights_at, slots = None, 0
     if weights is not None:
         weights_at, slots = _tracked(weights, "weights", torch.float32, device, n, kv_heads, None)
-    a = _pack_attn(TYPES[q.dtype], heads, kv_heads, dim, dim ** -0.5 if scale is None else scale, 0)
+    scale = dim ** -0.5 if scale is None else max(min(scale, 3e38), -3e38)       # (the library refuses what is too large for it)
+    a = _pack_attn(TYPES[q.dtype], heads, kv_heads, dim, scale, 0)
     need = 0
     if workspace is None:
         need = ibp_attn_decode4_workspace(n, heads, kv_heads, dim, max_len, weights is not None)

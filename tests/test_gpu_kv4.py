@@ -233,6 +233,41 @@ def test_decode_groups_of_nan(ibp, kind):
         assert torch.equal(lse[1], clean_lse[1]) and torch.equal(out[0, 2:], clean[0, 2:]) and torch.equal(out[1], clean[1])
 
 
+@pytest.mark.parametrize("kind", [BF16, F16])
+def test_decode_queries_that_are_not_finite(ibp, kind):
+    """Their own heads' results are NaN, and no other's."""
+    c = Cache(kind, 2, 128, [150, 90], 16, seed=18)
+    q = queries(c, 8)
+    before = torch.rand(2, 2, 150)
+    clean, clean_lse, clean_w = decode(ibp, c, q, before)
+    for bad in (float("inf"), float("-inf"), float("nan")):
+        x = q.clone()
+        x[0, 1, 77] = bad
+        out, lse, w = decode(ibp, c, x, before)
+        assert out[0, 1].isnan().all() and lse[0, 1].isnan()
+        rest = torch.ones(2, 8, dtype=torch.bool)
+        rest[0, 1] = False
+        assert torch.equal(out[rest], clean[rest]) and torch.equal(lse[rest], clean_lse[rest])
+        assert torch.equal(w[1], clean_w[1]) and torch.equal(w[0, 1], clean_w[0, 1])
+
+
+def test_two_streams_at_once(ibp):
+    """Two decodes with workspaces of their own, and an append, on streams of their own: each as alone."""
+    c = [Cache(BF16, 2, 128, [3000, 500], 32, seed=s) for s in (19, 20)]
+    q = [queries(x, 8, s).cuda() for s, x in enumerate(c)]
+    tensors = [(x.keys.cuda(), x.values.cuda(), x.table.cuda(), int32(x.lens)) for x in c]
+    want = [decode(ibp, x, y.cpu()) for x, y in zip(c, q)]
+    streams = [torch.cuda.Stream() for _ in c]
+    outs = [(torch.zeros_like(y), torch.zeros(2, 8, device="cuda")) for y in q]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for x, y, s, (o, lse) in zip(tensors, q, streams, outs):
+            ibp.ibp_attn_decode4(y, *x, 3000, o, lse, stream=s)
+    torch.cuda.synchronize()
+    for (o, lse), w in zip(outs, want):
+        assert torch.equal(o.cpu(), w[0]) and torch.equal(lse.cpu(), w[1])
+
+
 def test_decode_layouts(ibp):
     c = Cache(BF16, 4, 64, [90, 40], 16, seed=6)
     q = queries(c, 8)
@@ -554,7 +589,7 @@ def test_refusals(ibp):
                        (ValueError, dict(weights=torch.zeros(1, 3, 40, device="cuda"))), (TypeError, dict(lse=torch.zeros(1, 4, device="cuda", dtype=F16))),
                        (ibp.IbpError, dict(weights=torch.zeros(1, 2, 39, device="cuda"))),
                        (ibp.IbpError, dict(weights=torch.zeros(1, 2, 40, device="cuda"), workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))),
-                       (ibp.IbpError, dict(scale=0.0))]:
+                       (ibp.IbpError, dict(scale=0.0)), (ibp.IbpError, dict(scale=1e39)), (ibp.IbpError, dict(scale=float("nan")))]:
         with pytest.raises(error):
             ibp.ibp_attn_decode4(**{**base, **bad})
     rows = torch.empty(40, 2, 64, dtype=BF16, device="cuda")
