@@ -19,7 +19,7 @@
 // the next half chunk on their way (131,071 slots of 8 heads of 128: 41 us of which 7 are a block's start and end, 168 MB, 4.9 TB/s
 // in between; vector unit busy 0.62, LDS 0.38, matrix unit 0.17). Three waves a SIMD hide what a wave waits for its products; two, as
 // heads above 128 have them, took 41.5 instead of 37.5 us there when that was chosen. 64 sequences of up to 8,192 slots with the slots'
-// weights: 95 us (3.9 TB/s). Short caches are bound by one wave's instructions, one after another at some 8 cycles: 1,531 slots 8 us.
+// weights: 95 us (4.1 TB/s). Short caches are bound by one wave's instructions, one after another at some 8 cycles: 1,531 slots 8 us.
 #include <algorithm>
 #include <type_traits>
 
