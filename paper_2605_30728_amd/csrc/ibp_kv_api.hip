@@ -2,6 +2,8 @@
 // one or two launches on the caller's stream. Nothing is allocated, copied or synchronized here.
 #include <hip/hip_runtime.h>
 
+#include <string>
+
 #include "ibp_attn_checks.hpp"
 #include "ibp_kv_cache.hpp"
 
@@ -9,6 +11,21 @@ namespace ibp {
 namespace {
 
 using namespace attn;
+
+// What is written must not lie in itself: no two rows, heads, pages or slots of it in the same place, as a stride of 0 has them
+// (queries turned in place would be turned again and again).
+bool apart(int64_t stride, uint64_t count, uint32_t width) { return count <= 1 || stride >= (int64_t)width; }
+ibp_status take_apart(const Rows &r, uint64_t rows, uint32_t heads, uint32_t width, const char *what) {
+    if (!rows || (apart(r.row, rows, width) && apart(r.head, heads, width))) return IBP_OK;
+    return fail(IBP_EINVAL, std::string(what) + ": rows and heads that are written must not overlap");
+}
+ibp_status take_apart(const Pages &g, uint32_t heads, uint32_t width) {
+    if (!g.n_pages) return IBP_OK;
+    for (const attn::Pool &p : {g.k, g.v})
+        if (!apart(p.page, g.n_pages, width) || !apart(p.head, heads, width) || !apart(p.token, g.page_tokens, width))
+            return fail(IBP_EINVAL, "pages, heads and slots that are written must not overlap");
+    return IBP_OK;
+}
 
 // Packed rows of n_seqs sequences, or one row per sequence where there are no starts.
 ibp_status take_packed(const int32_t *d_starts, uint32_t n_seqs, uint64_t rows, const ibp_pages *pages) {
@@ -36,6 +53,7 @@ ibp_status append_impl(bool four, const ibp_attn *p, const ibp_rows *k, const ib
         if (q_out->rows < q->rows) return fail(IBP_ENOMEM, "q_out has fewer rows than q");
         if (q_out->data == q->data && (q_out->row_stride != q->row_stride || q_out->head_stride != q->head_stride))
             return fail(IBP_EINVAL, "in place q and q_out must have the same strides");
+        IBP_TRY(take_apart(a.q_out, q->rows, s.q_heads, s.dim, "q_out"));
     }
     if (rotation && rotation->turned) {
         if (rotation->turned % 8 || rotation->turned > s.dim) return fail(IBP_EINVAL, "turned values must be a multiple of 8, at most head_dim");
@@ -48,6 +66,7 @@ ibp_status append_impl(bool four, const ibp_attn *p, const ibp_rows *k, const ib
         a.halves = rotation->halves != 0;
     }
     IBP_TRY(take_pages(pages, 0, a.pg));
+    IBP_TRY(take_apart(a.pg, s.kv_heads, four ? record_bytes(s.dim) / 2 : s.dim));
     IBP_TRY(take_packed(d_starts, n_seqs, k->rows, pages));
     if (n_seqs && (!d_lens || !d_next)) return fail(IBP_EINVAL, "sequence lengths are null");
     if (!aligned(d_lens, 4) || !aligned(d_next, 4) || !aligned(d_weights, 4) || !aligned(d_positions, 4))
@@ -76,6 +95,8 @@ ibp_status read4_impl(const ibp_attn *p, const ibp_pages *pages, const int32_t *
     IBP_TRY(take_rows(k, "k", r.k));
     IBP_TRY(take_rows(v, "v", r.v));
     if (v->rows != k->rows) return fail(IBP_EINVAL, "k and v must have the same rows");
+    IBP_TRY(take_apart(r.k, k->rows, s.kv_heads, s.dim, "k"));
+    IBP_TRY(take_apart(r.v, v->rows, s.kv_heads, s.dim, "v"));
     IBP_TRY(take_pages(pages, 0, r.pg));
     IBP_TRY(take_packed(d_starts, n_seqs, k->rows, pages));
     if (n_seqs && !d_lens) return fail(IBP_EINVAL, "sequence lengths are null");
@@ -102,6 +123,7 @@ ibp_status decode4_impl(const ibp_attn *p, const ibp_rows *q, const ibp_pages *p
     IBP_TRY(take_rows(q, "q", rq));
     IBP_TRY(take_rows(out, "out", ro));
     if (out->rows < q->rows) return fail(IBP_ENOMEM, "out has fewer rows than q");
+    IBP_TRY(take_apart(ro, q->rows, s.q_heads, s.dim, "out"));
     IBP_TRY(take_pages(pages, max_len, pg));
     IBP_TRY(check_paged((uint32_t)q->rows, s.kv_heads, d_lens));
     if (d_weights && weights_stride < max_len) return fail(IBP_ENOMEM, "weights have fewer slots than max_len");

@@ -134,6 +134,24 @@ def test_decode_refuses():
     assert status("ibp_attn_decode4_workspace", 8, 4, 2, 64, 20, 1, None) == ibp.IBP_EINVAL
 
 
+@pytest.mark.parametrize("bad", [dict(row_stride=0), dict(head_stride=0), dict(row_stride=56), dict(head_stride=56)], ids=name)
+def test_outputs_that_lie_in_themselves_are_refused(bad):
+    """An expanded tensor has a stride of 0: as an input it is read, as an output two rows would be one."""
+    four = rows(heads=4, **bad)
+    for call in ("ibp_kv_append", "ibp_kv4_append"):
+        assert append(call, q=four, q_out=four) == ibp.IBP_EINVAL and append(call, q_out=rows(heads=4, data=2 * A, **bad)) == ibp.IBP_EINVAL
+        none = dict(k=rows(0), v=rows(0), q=rows(0, heads=4, row_stride=0), q_out=rows(0, heads=4, row_stride=0))
+        assert append(call, **none) == ibp.IBP_OK
+    assert read(k=rows(**bad)) == ibp.IBP_EINVAL and read(v=rows(**bad)) == ibp.IBP_EINVAL
+    assert decode(q=four, out=four) == ibp.IBP_EINVAL
+    one = dict(k=rows(0), v=rows(0), q=None, q_out=None)
+    wide = lambda x: {k: bad["row_stride"] if "row_stride" in bad else bad["head_stride"] for k in x}  # noqa: E731
+    for which in ("kp", "kh", "kt", "vp", "vh", "vt"):
+        assert append(g=pages(**wide([which])), **one) == ibp.IBP_EINVAL
+        assert append("ibp_kv4_append", g=pages(**{**wide([which]), which: min(wide([which])[which], 16)}), **one) == ibp.IBP_EINVAL
+    assert append(g=pages(n_pages=1, page_tokens=1, kp=0, kt=0, vp=0, vt=0), **one) == ibp.IBP_OK
+
+
 @pytest.mark.parametrize("weights", [False, True])
 @pytest.mark.parametrize("heads,kv_heads,dim", [(32, 8, 128), (8, 1, 256), (6, 2, 64), (16, 16, 80), (600, 600, 8), (64, 1, 128)])
 def test_decode_workspace_is_enough_for_smaller_calls(heads, kv_heads, dim, weights):
