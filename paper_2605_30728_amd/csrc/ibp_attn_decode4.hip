@@ -15,6 +15,12 @@
 // down to 2^-28 of the largest step and are there down to 2^-39. A float16 cache's are two bfloat16 parts, 16 bits at any
 // size (for a bfloat16 cache that took 45 us).
 //
+// Centres meet weights that are rounded less: values may lie in their centres alone, with signs by which sums are far below what is
+// added up (weights of 8 bits were off by 0.005 of such an output, more than its own rounding). A bfloat16 cache's are two bfloat16
+// parts, 16 bits at any size, side by side along one product's k of 32 (131,071 slots 47.9 us a call, 45.8 with one part).
+// float16 has too few exponents for parts: those weights stay in 32 bits, and so does the product (24 sequences of heads of 256 up
+// to 6,000 slots 26.6 us a call, 26.0 with weights of 16 bits; in the bfloat16 case above it took 50.9).
+//
 // A chunk of 64 slots is about 700 vector instructions and 52 matrix ones for a head of 128, with the records' loads of
 // the next half chunk on their way (131,071 slots of 8 heads of 128: 41 us of which 7 are a block's start and end, 168 MB, 4.9 TB/s
 // in between; vector unit busy 0.62, LDS 0.38, matrix unit 0.17). Three waves a SIMD hide what a wave waits for its products; two, as
@@ -83,6 +89,9 @@ __device__ __forceinline__ u32x2 read_codes(const uint8_t *p) {
 __device__ __forceinline__ u32x2 read_numbers(const uint8_t *p) {
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((IBP_LDS(s16x4) *)p));
 }
+
+// 16x16x4 of 32-bit numbers: A and B have k = l / 16, one number a lane; C as of the other products of 16 rows.
+__device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
 // The largest of x over a wave.
 __device__ __forceinline__ float max_wave(float x) {
@@ -344,10 +353,6 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 3 : 2) void k_attn_decode4(De
 
         store(now, true);
         if (chunk + kStep < to) load_keys(chunk + kStep);
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-            z = T::mfma16(read_numbers(meta + slot_of(t, quarter * 4 + (col >> 2)) * R::kMetaRow + (col & 3) * 8),
-                          u32x2{T::pack(s[t][0], s[t][1]), T::pack(s[t][2], s[t][3])}, z);
         const uint8_t *transposed = tile + slot_of(col >> 2, quarter * 4 + (col & 3)) * R::kRow;
         constexpr uint32_t minus = kHalf ? 0xc1bcc1bcu : 0xcde0cde0u;     // -47/2
         const Frag less = Frag{minus, minus, minus, minus};
@@ -378,6 +383,21 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 3 : 2) void k_attn_decode4(De
                     }
                 }
                 acc[g * 2 + half] = o;
+            }
+        }
+        // the centres, last: mixed with the products above their weights cost registers (20 spilled at heads of 128 in bfloat16)
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const u32x2 x = read_numbers(meta + slot_of(t, quarter * 4 + (col >> 2)) * R::kMetaRow + (col & 3) * 8);
+            if constexpr (kHalf) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z = mfma_f32(i % 2 ? high<T>(x[i / 2]) : low<T>(x[i / 2]), s[t][i], z);
+            } else {
+                const u32x2 p = {T::pack(s[t][0], s[t][1]), T::pack(s[t][2], s[t][3])};
+                z = T::mfma16(Frag{x[0], x[1], x[0], x[1]},
+                              Frag{p[0], p[1], T::pack(s[t][0] - low<T>(p[0]), s[t][1] - high<T>(p[0])),
+                                   T::pack(s[t][2] - low<T>(p[1]), s[t][3] - high<T>(p[1]))}, z);
             }
         }
     }
