@@ -587,7 +587,8 @@ ibp_status ibp_kv4_append(const ibp_attn *a, const ibp_rows *k, const ibp_rows *
 /*
  * ibp_kv4_read -- what slots d_first[s], d_first[s] + 1, ... (d_first null: 0, 1, ...) of a 4-bit cache stand for, into
  * rows d_starts[s], d_starts[s] + 1, ... of k and v (d_starts null: one row per sequence), values rounded
- * to fp32 and then to the type. Rows are left as they are from slot d_lens[s] or row d_starts[s + 1] on, where a
+ * to fp32 and then to the type; those past the type's largest number are that number where step and centre are
+ * finite (the ends of a group that holds it may be, by up to the step's rounding). Rows are left as they are from slot d_lens[s] or row d_starts[s + 1] on, where a
  * slot's page is absent, and outside all sequences: so a history is read to the front of a sequence's rows
  * whose last ones hold the new turn.
  */
