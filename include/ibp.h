@@ -561,8 +561,8 @@ typedef struct {
  * new slots (those below stride). A row whose slot is negative, beyond the table or of an absent page is not
  * appended (its query is turned all the same). Rows outside all sequences are left out. Slots
  * must be distinct: no page may be written for two sequences. Of `a` the type and heads are used (a valid scale still
- * given). No output may overlap an input otherwise, nor rows, heads, pages or slots of one another (their strides are
- * at least what they hold, or IBP_EINVAL).
+ * given). No output may overlap an input otherwise, nor rows, heads, pages or slots of one another: in the order of their
+ * strides each is at least what those before it span, or IBP_EINVAL.
  */
 ibp_status ibp_kv_append(const ibp_attn *a, const ibp_rows *k, const ibp_rows *v, const ibp_rows *q, const ibp_rows *q_out,
                          const ibp_rotation *rotation, const int32_t *d_starts, uint32_t n_seqs, const ibp_pages *pages,

@@ -2,6 +2,7 @@
 // one or two launches on the caller's stream. Nothing is allocated, copied or synchronized here.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <string>
 
 #include "ibp_attn_checks.hpp"
@@ -13,16 +14,31 @@ namespace {
 using namespace attn;
 
 // What is written must not lie in itself: no two rows, heads, pages or slots of it in the same place, as a stride of 0 has them
-// (queries turned in place would be turned again and again).
-bool apart(int64_t stride, uint64_t count, uint32_t width) { return count <= 1 || stride >= (int64_t)width; }
+// or rows as far apart as the heads (queries turned in place would be turned again and again). From the smallest stride on, each is
+// at least what those before it span; that takes any order of the dimensions, padding, and outputs in turns.
+struct Dim {
+    int64_t stride;
+    uint64_t count;
+};
+template <size_t N>
+bool apart(Dim (&&dims)[N], uint32_t width) {
+    std::sort(dims, dims + N, [](const Dim &x, const Dim &y) { return x.stride < y.stride; });
+    __int128 span = width;               // (2^31 pages of 2^40 values each do not fit 64 bits)
+    for (const Dim &d : dims) {
+        if (d.count <= 1) continue;
+        if (d.stride < span) return false;
+        span += (__int128)d.stride * (d.count - 1);
+    }
+    return true;
+}
 ibp_status take_apart(const Rows &r, uint64_t rows, uint32_t heads, uint32_t width, const char *what) {
-    if (!rows || (apart(r.row, rows, width) && apart(r.head, heads, width))) return IBP_OK;
+    if (!rows || apart({{r.row, rows}, {r.head, heads}}, width)) return IBP_OK;
     return fail(IBP_EINVAL, std::string(what) + ": rows and heads that are written must not overlap");
 }
 ibp_status take_apart(const Pages &g, uint32_t heads, uint32_t width) {
     if (!g.n_pages) return IBP_OK;
     for (const attn::Pool &p : {g.k, g.v})
-        if (!apart(p.page, g.n_pages, width) || !apart(p.head, heads, width) || !apart(p.token, g.page_tokens, width))
+        if (!apart({{p.page, g.n_pages}, {p.head, heads}, {p.token, g.page_tokens}}, width))
             return fail(IBP_EINVAL, "pages, heads and slots that are written must not overlap");
     return IBP_OK;
 }

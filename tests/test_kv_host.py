@@ -152,6 +152,55 @@ def test_outputs_that_lie_in_themselves_are_refused(bad):
     assert append(g=pages(n_pages=1, page_tokens=1, kp=0, kt=0, vp=0, vt=0), **one) == ibp.IBP_OK
 
 
+OVERLAPS = [dict(row_stride=64, head_stride=64), dict(row_stride=128, head_stride=64), dict(row_stride=192, head_stride=128),
+            dict(row_stride=64, head_stride=448), dict(row_stride=72, head_stride=64)]
+
+
+@pytest.mark.parametrize("bad", OVERLAPS, ids=name)
+def test_rows_and_heads_that_lie_in_each_other_are_refused(bad):
+    """Strides that hold a head each, by which one row's head is another row's: eight rows of four heads of 64."""
+    four = rows(heads=4, **bad)
+    heads4 = attn(kv_heads=4)
+    for call in ("ibp_kv_append", "ibp_kv4_append"):
+        none = dict(n=0, lens=None, nxt=None, starts=A)                   # (nothing would be launched)
+        assert append(call, q=four, q_out=four, **none) == ibp.IBP_EINVAL
+        assert append(call, q_out=rows(heads=4, data=2 * A, **bad), **none) == ibp.IBP_EINVAL
+        assert append(call, a=heads4, q=None, q_out=None, k=four, v=four, g=pages(n_pages=0), **none) == ibp.IBP_OK      # read alone
+    assert read(a=heads4, n=0, k=four, v=rows(heads=4)) == ibp.IBP_EINVAL and read(a=heads4, n=0, v=four, k=rows(heads=4)) == ibp.IBP_EINVAL
+    assert decode(q=four, out=four) == ibp.IBP_EINVAL
+
+
+BAD_POOLS = [dict(kp=64), dict(kp=1024), dict(kp=1984), dict(kh=512), dict(kt=128), dict(vp=1088), dict(vh=64, vt=64), dict(kp=1 << 40, kh=1 << 39, kt=1 << 39)]
+
+
+@pytest.mark.parametrize("bad", BAD_POOLS, ids=name)
+def test_pools_that_lie_in_themselves_are_refused(bad):
+    none = dict(n=0, lens=None, nxt=None, q=None, q_out=None)
+    assert append(g=pages(**bad), **none) == ibp.IBP_EINVAL
+    four = {k: x // 64 * 24 if x < 1 << 39 else x for k, x in {**dict(kp=2048, kh=1024, kt=64, vp=2048, vh=1024, vt=64), **bad}.items()}
+    assert append("ibp_kv4_append", g=pages(**four), **none) == ibp.IBP_EINVAL
+
+
+def test_layouts_that_lie_apart_are_taken():
+    """Any order of rows and heads, or of pages, heads and slots; keys and values in turns; padding; single ones of any stride."""
+    none = dict(n=0, lens=None, nxt=None)
+    for good in (dict(row_stride=256, head_stride=64), dict(row_stride=64, head_stride=512), dict(row_stride=320, head_stride=72),
+                 dict(row_stride=1 << 23, head_stride=64), dict(row_stride=64, head_stride=1 << 40)):
+        four = rows(heads=4, **good)
+        for call in ("ibp_kv_append", "ibp_kv4_append"):
+            assert append(call, q=four, q_out=four, g=pages(n_pages=0), **none) == ibp.IBP_OK
+        assert read(a=attn(kv_heads=4), n=0, k=four, v=four) == ibp.IBP_OK
+    assert append(q=rows(1, heads=4, row_stride=0), q_out=rows(1, heads=4, row_stride=0), k=rows(1), v=rows(1), **none) == ibp.IBP_OK
+    assert append(a=attn(q_heads=1, kv_heads=1), q=rows(heads=1, head_stride=0), q_out=rows(heads=1, head_stride=0), **none) == ibp.IBP_OK
+    orders = [dict(p=2048, h=1024, t=64), dict(p=2048, h=64, t=128), dict(p=4096, h=64, t=256), dict(p=64, h=256, t=512), dict(p=64, t=256, h=4096),
+              dict(p=1024, h=4096, t=64), dict(p=4096, h=1152, t=72), dict(p=1 << 40, h=1 << 39, t=64)]
+    for o in orders:
+        assert append(g=pages(**{"k" + d: x for d, x in o.items()}, **{"v" + d: x for d, x in o.items()}), q=None, q_out=None, **none) == ibp.IBP_OK
+    # (the largest counts and strides do not wrap around)
+    assert append(g=pages(n_pages=0x7fffff00, page_tokens=1 << 24, kp=1 << 40, kh=1 << 39, vp=1 << 40, vh=1 << 39), q=None, q_out=None, **none) == ibp.IBP_OK
+    assert append(g=pages(n_pages=0x7fffff00, page_tokens=1 << 24, kp=1 << 39, kh=1 << 40), q=None, q_out=None, **none) == ibp.IBP_EINVAL
+
+
 @pytest.mark.parametrize("weights", [False, True])
 @pytest.mark.parametrize("heads,kv_heads,dim", [(32, 8, 128), (8, 1, 256), (6, 2, 64), (16, 16, 80), (600, 600, 8), (64, 1, 128)])
 def test_decode_workspace_is_enough_for_smaller_calls(heads, kv_heads, dim, weights):
