@@ -50,7 +50,10 @@ def _taking(name):
 _KV_APPEND, _KV4_APPEND, _KV4_READ, _DECODE4 = (_taking(f) for f in ("ibp_kv_append", "ibp_kv4_append", "ibp_kv4_read", "ibp_attn_decode4"))
 _pack_attn, _pack_rows, _pack_pages, _pack_rotation = (struct.Struct(x).pack for x in ("4IfI", "4Q", "3Q2I7Q", "2Q2I"))
 assert all(struct.calcsize(x) == ctypes.sizeof(y) for x, y in (("4IfI", ibp_attn), ("4Q", ibp_rows), ("3Q2I7Q", ibp_pages), ("2Q2I", ibp_rotation)))
-_raw_stream = torch._C._cuda_getCurrentRawStream
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+if _raw_stream is None:                              # (a torch that has no handles without Stream objects around them)
+    def _raw_stream(device):
+        return torch.cuda.current_stream(device).cuda_stream
 
 
 def _device_of(x, what):

@@ -259,3 +259,28 @@ def test_the_operators_are_reached_from_module_and_package(first):
     root = os.path.dirname(os.path.dirname(os.path.abspath(ibp.__file__)))
     done = subprocess.run([sys.executable, "-c", f"{first}; print(f(128))"], cwd=root, capture_output=True, text=True)
     assert (done.returncode, done.stdout.strip()) == (0, "80"), done.stderr
+
+
+def test_the_module_needs_no_private_name_of_torch():
+    """What a torch without GPU support may lack is asked for when it is there, and the public calls otherwise."""
+    code = """
+import torch
+for name in [x for x in ("_cuda_getCurrentRawStream", "_cuda_getDevice") if hasattr(torch._C, x)]:
+    delattr(torch._C, name)
+import paper_2605_30728_amd as ibp
+from paper_2605_30728_amd import kv_cache as kc
+print(ibp.ibp_kv4_record(128), kc.ibp_kv_append is ibp.ibp_kv_append)
+k = torch.zeros(1, 1, 8, dtype=torch.bfloat16)
+i = torch.zeros(1, 1, dtype=torch.int32)
+try:
+    ibp.ibp_kv_append(k, k, k[None], k[None], i, i[0], i[0])
+except TypeError as e:
+    print(e)
+class Stream:
+    cuda_stream = 77
+torch.cuda.current_stream = lambda device: Stream
+print(kc._raw_stream(0))
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(ibp.__file__)))
+    done = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True)
+    assert (done.returncode, done.stdout.splitlines()) == (0, ["80 True", "k must be a GPU tensor", "77"]), done.stderr
