@@ -56,6 +56,10 @@ if _raw_stream is None:                              # (a torch that has no hand
         return torch.cuda.current_stream(device).cuda_stream
 
 
+def _beyond(what, *sizes):
+    return ValueError(f"{what} must fit 32 bits, not {', '.join(str(x) for x in sizes)}")
+
+
 def _device_of(x, what):
     try:
         device = x.get_device()                      # (-1 for a host tensor)
@@ -118,7 +122,10 @@ def _pool_of(keys, values, table, device, kind, unit, kv_heads, width, what):
         raise ValueError("table must be [sequences][pages]") from None
     if unit == 2:
         a, b, c, e, f, g = a >> 1, b >> 1, c >> 1, e >> 1, f >> 1, g >> 1
-    return sequences, _pack_pages(keys.data_ptr(), values.data_ptr(), n, t, pages, table.data_ptr(), a, b, c, e, f, g)
+    try:
+        return sequences, _pack_pages(keys.data_ptr(), values.data_ptr(), n, t, pages, table.data_ptr(), a, b, c, e, f, g)
+    except struct.error:
+        raise _beyond("slots of a page and pages of a sequence", t, pages) from None
 
 
 def _wrong_pools(keys, values, device, kind, kv_heads, width, what):
@@ -133,6 +140,8 @@ def _wrong_pools(keys, values, device, kind, kv_heads, width, what):
 
 def _sequences(n, lens, starts, rows, device):
     """The addresses of n sequences' lengths and starts."""
+    if n >> 32:
+        raise _beyond("sequences", n)
     lens_at = _numbers(lens, "lens", torch.int32, device, (n,))
     if starts is None:
         if rows != n:
@@ -170,14 +179,21 @@ def _appender(call, name, four, about):
             at = _numbers(rotation, "rotation", torch.float32, device, shape)
             if len(shape) != 3 or shape[2] != 2:
                 raise ValueError("rotation must be [positions][pairs][2]")
-            turn = _pack_rotation(at, shape[0], 2 * shape[1], 1 if halves else 0)
+            try:
+                turn = _pack_rotation(at, shape[0], 2 * shape[1], 1 if halves else 0)
+            except struct.error:
+                raise _beyond("values that a rotation turns", 2 * shape[1]) from None
         slots, weights_at, positions_at = 0, None, None
         if weights is not None:
             weights_at, slots = _tracked(weights, "weights", torch.float32, device, n, kv_heads, None)
         if positions is not None:
             positions_at, slots = _tracked(positions, "positions", torch.int32, device, n, kv_heads, slots if weights is not None else None)
-        status = call(_pack_attn(TYPES[kind], heads, kv_heads, dim, 1.0, 0), rk, rv, rq, ro, turn, starts_at, n, pages, lens_at, next_at,
-                      weights_at, positions_at, slots, _raw_stream(device) if stream is None else _stream(stream, device))
+        try:
+            a = _pack_attn(TYPES[kind], heads, kv_heads, dim, 1.0, 0)
+        except struct.error:
+            raise _beyond("heads and head_dim", heads, kv_heads, dim) from None
+        status = call(a, rk, rv, rq, ro, turn, starts_at, n, pages, lens_at, next_at, weights_at, positions_at,
+                      slots, _raw_stream(device) if stream is None else _stream(stream, device))
         if status:
             check(status, name)
 
@@ -229,7 +245,11 @@ def ibp_kv4_read(keys, values, table, lens, k, v, starts=None, first=None, strea
     n, pages = _pool_of(keys, values, table, device, torch.uint8, 2, kv_heads, ibp_kv4_record(dim), "records")
     lens_at, starts_at = _sequences(n, lens, starts, rows, device)
     first_at = None if first is None else _numbers(first, "first", torch.int32, device, (n,))
-    status = _KV4_READ(_pack_attn(TYPES[kind], kv_heads, kv_heads, dim, 1.0, 0), pages, lens_at, n, starts_at, first_at, rk, rv,
+    try:
+        a = _pack_attn(TYPES[kind], kv_heads, kv_heads, dim, 1.0, 0)
+    except struct.error:
+        raise _beyond("heads and head_dim", kv_heads, dim) from None
+    status = _KV4_READ(a, pages, lens_at, n, starts_at, first_at, rk, rv,
                        _raw_stream(device) if stream is None else _stream(stream, device))
     if status:
         check(status, "ibp_kv4_read")
@@ -262,7 +282,10 @@ def ibp_attn_decode4(q, keys, values, table, lens, max_len, out, lse=None, weigh
     if weights is not None:
         weights_at, slots = _tracked(weights, "weights", torch.float32, device, n, kv_heads, None)
     scale = dim ** -0.5 if scale is None else max(min(scale, 3e38), -3e38)       # (the library refuses what is too large for it)
-    a = _pack_attn(TYPES[q.dtype], heads, kv_heads, dim, scale, 0)
+    try:
+        a = _pack_attn(TYPES[q.dtype], heads, kv_heads, dim, scale, 0)
+    except struct.error:
+        raise _beyond("heads and head_dim", heads, kv_heads, dim) from None
     need = 0
     if workspace is None:
         need = ibp_attn_decode4_workspace(n, heads, kv_heads, dim, max_len, weights is not None)

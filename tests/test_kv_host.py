@@ -284,3 +284,23 @@ print(kc._raw_stream(0))
     root = os.path.dirname(os.path.dirname(os.path.abspath(ibp.__file__)))
     done = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True)
     assert (done.returncode, done.stdout.splitlines()) == (0, ["80 True", "k must be a GPU tensor", "77"]), done.stderr
+
+
+def test_binding_refuses_counts_beyond_32_bits():
+    """Shapes alone (meta tensors have no data): a count that the library takes in 32 bits is neither cut nor an error of the packing."""
+    def meta(*shape, kind=torch.int32):
+        return torch.empty(shape, dtype=kind, device="meta")
+    big = (1 << 32) + 1
+    with pytest.raises(ValueError, match="sequences must fit 32 bits"):
+        kc._sequences(big, meta(big), meta(big + 1), 5, -1)
+    with pytest.raises(ValueError, match="sequences must fit 32 bits"):
+        kc._sequences(big, meta(big), None, big, -1)
+    kc._sequences(7, meta(7), meta(8), 5, -1)
+
+    def pool(page, pages):
+        x = meta(1, 1, page, 32, kind=torch.uint8)
+        return kc._pool_of(x, x, meta(2, pages), -1, torch.uint8, 2, 1, 32, "records")
+    assert pool((1 << 32) - 1, 1)[0] == pool(1, (1 << 32) - 1)[0] == 2
+    for page, pages in ((1 << 32, 1), (1, 1 << 32)):
+        with pytest.raises(ValueError, match="32 bits"):
+            pool(page, pages)
