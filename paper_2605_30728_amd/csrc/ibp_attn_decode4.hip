@@ -11,7 +11,7 @@
 // The weights times steps p_j step_jg are rounded for the product with the codes, and the same rounded ones meet 16 + c and 47/2. In
 // bfloat16 that would show as much as the rounding of the output does (error against 64 bits 0.0023 of the output instead of
 // 0.0017), so a bfloat16 cache's are float16 numbers (39 us for the long cache below instead of 37.5), its steps scaled so that
-// the largest so far is from 4 to 8 and weights lifted by 2^12 as float16 weights are elsewhere: they have 11 bits
+// the largest so far is from 2^14 to 2^15, which leaves float16's small numbers to small weights: they have 11 bits
 // down to 2^-28 of the largest step and are there down to 2^-39. A float16 cache's are two bfloat16 parts, 16 bits at any
 // size (for a bfloat16 cache that took 45 us).
 //
@@ -117,7 +117,6 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 3 : 2) void k_attn_decode4(De
     constexpr bool kHalf = std::is_same_v<T, F16>;
     using P = std::conditional_t<kHalf, Bf16, F16>;  // of the weights times steps, kParts numbers each
     constexpr int kParts = kHalf ? 2 : 1;
-    constexpr int kLift = F16::kLift;                // of the weights, until the slots are done
     constexpr int kJoin = 16 * (DIM + 4) * 4;        // a wave's sums, for the join
     constexpr int kWaveBytes = R::kBytes > kJoin ? R::kBytes : kJoin;
     __shared__ __align__(128) uint8_t lds[kWaves * kWaveBytes];
@@ -234,8 +233,10 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 3 : 2) void k_attn_decode4(De
         value_at = (pg * a.pg.v.page + (int64_t)place * a.pg.v.token) * 2;
         load(kbase, (pg * a.pg.k.page + (int64_t)place * a.pg.k.token) * 2);
     };
-    float down = 1.f, limit = 0.f;       // what a bfloat16 cache's value steps are scaled with, and what they are below
-    auto raise = [&](float top, const float (&step)[G]) {      // the largest step to 4 .. 8, and with it what there is so far
+    // A bfloat16 cache's value steps are scaled by 2^shift: the largest so far, which is below `limit`, to 2^14 .. 2^15.
+    int shift = 0;
+    float limit = 0.f;
+    auto raise = [&](float top, const float (&step)[G]) {      // a larger one, and with it what there is so far
         if (top == inf) {
             top = 0.f;
 #pragma unroll
@@ -243,14 +244,13 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 3 : 2) void k_attn_decode4(De
             top = max_wave(top);
             if (top < limit || top == 0.f) return;
         }
-        const int e = max((int)(__float_as_uint(top) >> 23) - 127, -120);
-        const float next = __builtin_amdgcn_ldexpf(1.f, 2 - e);
+        const int e = (int)(__float_as_uint(top) >> 23) - 127, next = 14 - e;
         if (limit > 0.f) {
-            const float less = next / down;
+            const float less = __builtin_amdgcn_ldexpf(1.f, next - shift);
 #pragma unroll
             for (int d = 0; d < DT; ++d) acc[d] *= less;
         }
-        down = next;
+        shift = next;
         limit = __builtin_amdgcn_ldexpf(2.f, e);
     };
     auto store = [&](uint64_t live, bool of_values) {
@@ -272,7 +272,7 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 3 : 2) void k_attn_decode4(De
             top = max_wave(top);
             if (top >= limit && top > 0.f) raise(top, step);
 #pragma unroll
-            for (int g = 0; g < G; ++g) step[g] *= down;
+            for (int g = 0; g < G; ++g) step[g] = __builtin_amdgcn_ldexpf(step[g], shift);
         }
 #pragma unroll
         for (int g = 0; g < G; ++g) steps[g * kChunk + lane] = step[g];
@@ -346,7 +346,7 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 3 : 2) void k_attn_decode4(De
         for (int t = 0; t < 4; ++t) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                s[t][i] = exp2_fast(__builtin_fmaf(s[t][i] - ref, c, (float)kLift));
+                s[t][i] = exp2_fast((s[t][i] - ref) * c);
                 l += s[t][i];
             }
         }
@@ -403,8 +403,7 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 3 : 2) void k_attn_decode4(De
     }
 
     // the block's waves joined: lane's column is a head, its registers dims quarter * 4 + i (of z: a record's numbers)
-    constexpr float unit = 1.f / (1 << kLift);
-    l = sum_halves(sum_quarters(l)) * unit;
+    l = sum_halves(sum_quarters(l));
     if (quarter == 0) {
         stat[wave][0][col] = m;
         stat[wave][1][col] = l;
@@ -413,8 +412,13 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 3 : 2) void k_attn_decode4(De
     __syncthreads();
     float *mine = reinterpret_cast<float *>(tile);
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
-        *reinterpret_cast<f32x4 *>(mine + col * (DIM + 4) + d * 16 + quarter * 4) = acc[d] * (unit / down) + sums[wave][col][G + d / 2] * unit;
+    for (int d = 0; d < DT; ++d) {
+        const float centre = sums[wave][col][G + d / 2];
+        f32x4 x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = (kHalf ? acc[d][i] : __builtin_amdgcn_ldexpf(acc[d][i], -shift)) + centre;
+        *reinterpret_cast<f32x4 *>(mine + col * (DIM + 4) + d * 16 + quarter * 4) = x;
+    }
     __syncthreads();
     const int h = threadIdx.x >> 4;          // 16 heads, 16 threads each
     if (h >= heads) return;

@@ -104,6 +104,40 @@ def test_sizes_of_centres(ibp, kind):
             assert (out[b, 0] > 0).all()
 
 
+@pytest.mark.parametrize("steps", [False, True])
+def test_values_far_above_one(ibp, steps):
+    """Of a bfloat16 cache whose values add up to nearly 2^128: what they stand for is finite, and so is the result."""
+    c = Cache(BF16, 2, 96, [1, 40, 130], 16, seed=10)
+    g = torch.Generator().manual_seed(11)
+    size = 2.0 ** 118
+    if steps:
+        fill(c, lambda n: torch.randn(n, 2, 96, generator=g).clamp(-3, 3) * size)
+    else:
+        fill(c, lambda n: (torch.randint(1, 4, (n, 2, 3, 1), generator=g) * size).expand(-1, -1, -1, 32).flatten(2))
+    q = sharp(c, 4, 12)
+    out, lse, _ = decode(ibp, c, q, scale=1.0)
+    assert out.isfinite().all()
+    check(c, q, out, lse)
+
+
+def test_steps_far_below_one(ibp):
+    """The smallest steps that a bfloat16 cache holds, with weights down to 2^-20: as precise as others."""
+    c = Cache(BF16, 2, 64, [1, 40, 1000], 16, seed=13)
+    g = torch.Generator().manual_seed(14)
+    for size in (2.0 ** -124, 2.0 ** -118, 2.0 ** -112):
+        fill(c, lambda n: torch.randn(n, 2, 64, generator=g) * size)
+        q = sharp(c, 4, 15, 4.0)
+        out, lse, _ = decode(ibp, c, q, scale=1.0)
+        for b, n in enumerate(c.lens):
+            for h in range(4):
+                keys, values = (c.rows(x, b, h // 2, range(n)) for x in (c.keys, c.values))
+                o, _, tol, _ = attend4(q[b, h], keys, values, 1.0)
+                p, _ = weights4(q[b, h], keys, 1.0)
+                tol = tol + 1.01 * 2.0 ** -17 * (p @ parts_of(values, 64, BF16)[2].abs())
+                # (a bfloat16 output below 2^-126 is off by up to half of 2^-133, and fp32 sums of such numbers by up to half of 2^-149 each)
+                assert ((out[b, h].double() - o).abs() <= tol + 2.0 ** -134 + 2 * n * 2.0 ** -150).all(), size
+
+
 @pytest.mark.parametrize("kind", [BF16, F16])
 @pytest.mark.parametrize("down", [25.0, 33.3, 36.3, 38.5])
 @pytest.mark.parametrize("heads", [1, 512])
