@@ -599,7 +599,7 @@ ibp_status ibp_kv4_read(const ibp_attn *a, const ibp_pages *pages, const int32_t
 /*
  * ibp_attn_decode4 -- ibp_attn_decode over a cache of records: keys and values are what these stand for, exactly.
  * Queries must be finite (else the head's results are NaN); a group whose step or centre is not finite
- * gives NaN where it is seen (keys) or in its own columns (values).
+ * gives NaN where it is seen (keys), or results that are not finite in its own columns (values).
  * A value's weight meets the group's step and its centre apart. Weights times steps have, in bfloat16 caches, 11 bits down to
  * 2^-28 of the largest step, fewer below, none under 2^-39 of it; in float16 caches 16 bits throughout. Weights of
  * centres have 16 bits in bfloat16 caches and are fp32 in float16 ones.

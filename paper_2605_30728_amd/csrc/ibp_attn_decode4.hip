@@ -10,22 +10,23 @@
 //
 // The weights times steps p_j step_jg are rounded for the product with the codes, and the same rounded ones meet 16 + c and 47/2. In
 // bfloat16 that would show as much as the rounding of the output does (error against 64 bits 0.0023 of the output instead of
-// 0.0017), so a bfloat16 cache's are float16 numbers (39 us for the long cache below instead of 37.5), its steps scaled so that
+// 0.0017), so a bfloat16 cache's are float16 numbers (39 us for the long cache below instead of 37.5 then), its steps scaled so that
 // the largest so far is from 2^14 to 2^15, which leaves float16's small numbers to small weights: they have 11 bits
 // down to 2^-28 of the largest step and are there down to 2^-39. A float16 cache's are two bfloat16 parts, 16 bits at any
-// size (for a bfloat16 cache that took 45 us).
+// size (for a bfloat16 cache that took 45 us then).
 //
 // Centres meet weights that are rounded less: values may lie in their centres alone, with signs by which sums are far below what is
 // added up (weights of 8 bits were off by 0.005 of such an output, more than its own rounding). A bfloat16 cache's are two bfloat16
-// parts, 16 bits at any size, side by side along one product's k of 32 (131,071 slots 47.9 us a call, 45.8 with one part).
-// float16 has too few exponents for parts: those weights stay in 32 bits, and so does the product (24 sequences of heads of 256 up
-// to 6,000 slots 26.6 us a call, 26.0 with weights of 16 bits; in the bfloat16 case above it took 50.9).
+// parts, 16 bits at any size, side by side along one product's k of 32 (131,071 slots 47.9 us a call when that was chosen, 45.8 with one
+// part, 50.9 with weights in 32 bits). float16 has too few exponents for parts: those weights stay in 32 bits, and so does the
+// product (24 sequences of heads of 256 up to 6,000 slots 26.6 us a call, 26.0 with weights of 16 bits).
 //
-// A chunk of 64 slots is about 700 vector instructions and 52 matrix ones for a head of 128, with the records' loads of
-// the next half chunk on their way (131,071 slots of 8 heads of 128: 41 us of which 7 are a block's start and end, 168 MB, 4.9 TB/s
-// in between; vector unit busy 0.62, LDS 0.38, matrix unit 0.17). Three waves a SIMD hide what a wave waits for its products; two, as
-// heads above 128 have them, took 41.5 instead of 37.5 us there when that was chosen. 64 sequences of up to 8,192 slots with the slots'
-// weights: 95 us (4.1 TB/s). Short caches are bound by one wave's instructions, one after another at some 8 cycles: 1,531 slots 8 us.
+// A chunk of 64 slots is about 730 vector instructions and 56 matrix ones for a head of 128 in bfloat16, with the records' loads of
+// the next half chunk on their way (131,071 slots of 8 heads of 128: 43 us of which some 7 are a block's start and end, 168 MB, 4.7 TB/s
+// in between; vector unit busy 0.63, LDS 0.36, matrix unit 0.17; in float16, with two parts and the centres in 32 bits, 56 us).
+// 64 sequences of up to 8,192 slots with the slots' weights: 97 us (4.0 TB/s; in float16 117). Three waves a SIMD hide what a wave waits
+// for its products; two, as heads above 128 have them, took 125 us a call there instead of 116 when that was measured. Short
+// caches are bound by one wave's instructions, one after another at some 8 cycles: 1,531 slots 8 us, no less than their 16-bit decode.
 #include <algorithm>
 #include <type_traits>
 
@@ -109,7 +110,8 @@ __device__ __forceinline__ float max_wave(float x) {
 // of all four products are spread over the banks.
 __device__ __forceinline__ int slot_of(int t, int row) { return t * 16 + (row ^ (t & 1) * 8); }
 
-// Three waves a SIMD for heads of up to 128, whose 168 registers hold what a wave has in work; of 256 values it is twice that.
+// Three waves a SIMD for heads of up to 128, two above, whose 168 and 256 registers hold what a wave has in work but for a few that
+// spill into the loop: nine of heads of 97 to 128 in float16, of heads above 224 eight in bfloat16 and 13 in float16.
 template <class T, int G>
 __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 3 : 2) void k_attn_decode4(DecodeArgs a) {
     using R = Rec<G>;
@@ -385,7 +387,7 @@ __global__ __launch_bounds__(64 * kWaves, G <= 4 ? 3 : 2) void k_attn_decode4(De
                 acc[g * 2 + half] = o;
             }
         }
-        // the centres, last: mixed with the products above their weights cost registers (20 spilled at heads of 128 in bfloat16)
+        // the centres, last: mixed with the products above their weights cost registers (heads of 128 in bfloat16 spilled 20)
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -485,9 +487,9 @@ constexpr uint32_t kManySplit = 768;                 // slots per split, where s
 DecodePlan plan_decode4(uint32_t n_seqs, uint32_t q_heads, uint32_t kv_heads, uint32_t dim, uint32_t max_len, bool weights) {
     DecodePlan p{};
     p.head_blocks = (q_heads / kv_heads + 15) / 16;
-    // a single sequence: about 512 blocks (131,071 slots of 8 heads of 128: first kernel 37.7 us, with 768 blocks 38.7, with 1,536
-    // 40.3 and a longer join). Several, whose lengths differ: up to 1,024 blocks, and more of 768 slots (64 sequences of
-    // up to 8,192 slots: 91 us, of 512 slots 95, of 1,536 95, of 2,048 94).
+    // a single sequence: about 512 blocks (131,071 slots of 8 heads of 128: 46.3 us a call, with 768 blocks 47.5, with 1,536
+    // 52.6). Several, whose lengths differ: up to 1,024 blocks, and more of 768 slots (64 sequences of
+    // up to 8,192 slots: 112.6 us a call, of 512 slots 114.3, of 1,536 119.2, of 2,048 117.6).
     const uint64_t rows = std::max<uint64_t>((uint64_t)n_seqs * kv_heads * p.head_blocks, 1), len = std::max<uint64_t>(max_len, 1);
     uint64_t t = n_seqs > 1 ? std::min<uint64_t>((len * rows + 1023) / 1024, kManySplit) : (len * rows + 511) / 512;
     t = std::max<uint64_t>(t, (len + kMaxSplits - 1) / kMaxSplits);

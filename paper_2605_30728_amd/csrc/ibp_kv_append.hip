@@ -6,10 +6,10 @@
 //   per 32 values  centre = type((lo + hi) / 2),  step = type(2/15 max(hi - centre, centre - lo)),
 //   code = round((x - centre) / step + 7.5) clamped to 0 .. 15,  value = centre + (code - 7.5) step.
 //
-// Large calls are bound by HBM: 8,192 rows of 32/8 heads of 128 in bfloat16 39 us into 16-bit pages (206 MB, 5.3 TB/s, as a large
+// Large calls are bound by HBM: 8,192 rows of 32/8 heads of 128 in bfloat16 39.5 us into 16-bit pages (206 MB, 5.2 TB/s, as a large
 // copy) and 45 into records (182 MB, 4.0 TB/s, with the conversions between the loads and the stores), 32,768 slots of 8 heads of
-// 128 read back 29 us (176 MB, 6.1 TB/s: 134 of them written around the caches). Small ones by the look-ups, each of
-// which waits for the one before (the row's sequence, its length, its page): one row 2.8 us, 64 rows 3.5, into records 4.6,
+// 128 read back 29.5 us (176 MB, 6.0 TB/s: 134 of them written around the caches). Small ones by the look-ups, each of
+// which waits for the one before (the row's sequence, its length, its page): one row 2.7 us, 64 rows 3.6, into records 4.6,
 // of which a launch is about 2.
 #include "ibp_attn_wave.hpp"
 #include "ibp_kv_cache.hpp"
@@ -198,7 +198,7 @@ __device__ __forceinline__ bool find_where(const Append &a, uint32_t row, Where 
 
 // Items, of eight values each, that a lane has on their way together: four fill the chip's memory system (8,192 rows appended 39 us,
 // with two 41.5, with eight 40; into records 45, with two 53). In calls of too few rows for that one each is sooner done
-// (64 rows 3.5 us instead of 5.5).
+// (64 rows 3.5 us instead of 5.5). Four into records keep 12 to 14 scalar registers in vector ones' lanes.
 constexpr int kMany = 4;
 constexpr uint64_t kFewWaves = 2048;     // (of so many items)
 
